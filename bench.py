@@ -47,7 +47,8 @@ def lib_digest():
     traffic figures measured on other code are not reported."""
     h = hashlib.sha256()
     csrc = os.path.join(ROOT, "paper_2608_26004_amd", "csrc")
-    # every source of libasymspec.so (the read-ceiling probe is its own library)
+    # every source of the decision step (csrc/step/ holds the operators around
+    # it; the read-ceiling probe is its own library)
     paths = sorted(os.path.join(csrc, n) for n in os.listdir(csrc)
                    if n.endswith((".hip", ".h")) and n != "probe.hip")
     for p in paths + [os.path.join(ROOT, "include", "asymspec.h")]:

@@ -11,7 +11,8 @@ from __future__ import annotations
 import ctypes
 import os
 
-__all__ = ["fuse_verify", "workspace_size", "Workspace", "load_library", "status_string",
+__all__ = ["fuse_verify", "shape_logits", "draw_tokens", "commit_tokens", "plan_slots",
+           "workspace_size", "Workspace", "load_library", "status_string",
            "workspace_timeouts", "set_wait_limit",
            "BF16", "FP32", "GATE_CDA", "GATE_FIXED", "GATE_KL", "GATE_LAMBDA",
            "DELTA_AB", "DELTA_A", "DELTA_TB", "FUSE_BONUS", "EARLY_EXIT", "AsymSpecError"]
@@ -255,3 +256,7 @@ def fuse_verify(t, a, b, draft_tokens, draft_probs, uniforms, temperature,
     if return_full:
         res += (full,)
     return res
+
+
+# the operators around the decision step
+from .step import commit_tokens, draw_tokens, plan_slots, shape_logits  # noqa: E402

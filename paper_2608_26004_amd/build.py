@@ -27,10 +27,10 @@ FLAGS = [
 
 def units():
     """(object name, source, defines) of every object of the library: the host
-    side, the cross-family kernels per storage type, and one object per
-    instance of the decision kernel (storage type x source of delta x variant),
-    compiled in parallel."""
-    out = [("asymspec", "asymspec.hip", [])]
+    side, the operators around the decision step, the cross-family kernels per
+    storage type, and one object per instance of the decision kernel (storage
+    type x source of delta x variant), compiled in parallel."""
+    out = [("asymspec", "asymspec.hip", []), ("step", os.path.join("step", "step.hip"), [])]
     for dt in (0, 1):
         out.append((f"xv_{dt}", "xvocab.hip", [f"-DASYMSPEC_PART_DT={dt}"]))
         for dm in (0, 1, 2):

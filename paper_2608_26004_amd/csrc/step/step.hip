@@ -1,0 +1,248 @@
+// The operators around the decision step (asymspec_step.h): host checks and
+// launches.  The kernels stand in shape.h, draw.h, commit.h and slots.h.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+
+#include "asymspec_step.h"
+#include "commit.h"
+#include "draw.h"
+#include "shape.h"
+#include "slots.h"
+
+namespace asym_step {
+
+static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+
+// Compute units of the current device, or 0 when it is no gfx950.
+static int device_cus() {
+  static std::mutex mu;
+  static int cus[64];       // 0: not looked at; -1: not a gfx950
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
+    (void)hipGetLastError();
+    return 0;
+  }
+  std::lock_guard<std::mutex> lk(mu);
+  if (cus[dev] == 0) {
+    hipDeviceProp_t pr;
+    if (hipGetDeviceProperties(&pr, dev) != hipSuccess) {
+      (void)hipGetLastError();
+      return 0;
+    }
+    cus[dev] = std::strncmp(pr.gcnArchName, "gfx950", 6) == 0 ? pr.multiProcessorCount : -1;
+  }
+  return std::max(cus[dev], 0);
+}
+
+static int launched() {
+  if (hipGetLastError() == hipSuccess) return ASYMSPEC_OK;
+  return ASYMSPEC_E_DEVICE;
+}
+
+// Whether the rows of a [B][R][V] tensor lie apart, in one order or the other,
+// and its last element within 2^62 of the first.
+static bool rows_apart(int64_t B, int64_t R, int64_t V, int64_t sb, int64_t sr) {
+  if (sb < 0 || sr < 0) return false;
+  const __int128 span = (__int128)(B - 1) * sb + (__int128)(R - 1) * sr + V;
+  if (span > ((__int128)1 << 60)) return false;
+  const bool request_major = (R == 1 || sr >= V) && (B == 1 || sb >= (R - 1) * sr + V);
+  const bool row_major = (B == 1 || sb >= V) && (R == 1 || sr >= (B - 1) * sb + V);
+  return request_major || row_major;
+}
+
+template <int DT>
+static void shape_launch(const ShapeArgs& A, unsigned grid, size_t lds, hipStream_t st) {
+  const bool in_place = A.s.logits == A.s.out, masked = A.s.mask != nullptr;
+  if (in_place && masked) shape_kernel<DT, true, true><<<grid, kShapeThreads, lds, st>>>(A);
+  else if (in_place) shape_kernel<DT, true, false><<<grid, kShapeThreads, lds, st>>>(A);
+  else if (masked) shape_kernel<DT, false, true><<<grid, kShapeThreads, lds, st>>>(A);
+  else shape_kernel<DT, false, false><<<grid, kShapeThreads, lds, st>>>(A);
+}
+
+// Workspace of a draw; chunks of a row in *S.  0 for invalid arguments.
+static size_t draw_bytes(int N, int V, int dtype, int* S) {
+  if (N < 1 || V < 1 || V >= (1 << 30) || (dtype != ASYMSPEC_BF16 && dtype != ASYMSPEC_FP32)) return 0;
+  *S = (V + kDrawChunk - 1) / kDrawChunk;
+  if ((long long)N * *S > 0x7FFFFFFFll) return 0;
+  return (size_t)N * *S * sizeof(DrawPart);
+}
+
+}  // namespace asym_step
+
+using namespace asym_step;
+
+extern "C" {
+
+int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
+  if (shape == nullptr) return ASYMSPEC_E_ARG;
+  ShapeArgs A;
+  A.s = *shape;
+  asymspec_shape& s = A.s;
+  if (s.dtype != ASYMSPEC_BF16 && s.dtype != ASYMSPEC_FP32) return ASYMSPEC_E_ARG;
+  if (s.B < 1 || s.R < 1 || s.R > ASYMSPEC_SHAPE_MAX_ROWS || s.V < 1) return ASYMSPEC_E_ARG;
+  if (s.logits == nullptr || s.out == nullptr) return ASYMSPEC_E_ARG;
+  // the row strides of one row, and the request strides of one request, do not matter
+  if (s.R == 1) s.row_stride = s.out_row_stride = 0;
+  if (s.B == 1) s.request_stride = s.out_request_stride = 0;
+  if (s.request_stride < 0 || s.row_stride < 0 || s.request_stride > (1ll << 40) || s.row_stride > (1ll << 40))
+    return ASYMSPEC_E_ARG;
+  if (!rows_apart(s.B, s.R, s.V, s.out_request_stride, s.out_row_stride)) return ASYMSPEC_E_ARG;
+  if (s.logits == s.out && (s.request_stride != s.out_request_stride || s.row_stride != s.out_row_stride))
+    return ASYMSPEC_E_ARG;
+  if (s.history != nullptr) {
+    if (s.lengths == nullptr || s.max_history < 1 || s.max_history > ASYMSPEC_SHAPE_MAX_HISTORY) return ASYMSPEC_E_ARG;
+  } else {
+    s.lengths = s.prompt_lengths = nullptr;
+    s.max_history = 0;
+  }
+  if (s.draft_tokens == nullptr) s.D = 0;
+  if (s.D < 0 || s.D > kShapeMaxDrafts || (s.D > 0 && s.D < s.R - 1)) return ASYMSPEC_E_ARG;
+  if (s.D > 0 && s.B > 1 && (s.draft_stride < 0 || s.draft_stride > (1ll << 40))) return ASYMSPEC_E_ARG;
+  if (s.B == 1) s.draft_stride = 0;
+  if (s.id_map != nullptr && s.n_ids < 0) return ASYMSPEC_E_ARG;
+  if ((s.bias_ids == nullptr) != (s.bias_values == nullptr)) return ASYMSPEC_E_ARG;
+  if (s.bias_ids == nullptr) s.n_bias = 0;
+  if (s.n_bias < 0 || s.n_bias > ASYMSPEC_SHAPE_MAX_BIAS) return ASYMSPEC_E_ARG;
+  if ((s.mask == nullptr) != (s.mask_index == nullptr)) return ASYMSPEC_E_ARG;
+  if (s.mask != nullptr && s.n_masks < 0) return ASYMSPEC_E_ARG;
+  const size_t el = s.dtype == ASYMSPEC_BF16 ? 2 : 4;
+  if (!aligned(s.logits, el) || !aligned(s.out, el)) return ASYMSPEC_E_ALIGN;
+  for (const void* p : {(const void*)s.history, (const void*)s.lengths, (const void*)s.prompt_lengths,
+                        (const void*)s.draft_tokens, (const void*)s.id_map, (const void*)s.repetition,
+                        (const void*)s.frequency, (const void*)s.presence, (const void*)s.bias_ids,
+                        (const void*)s.bias_values, (const void*)s.mask, (const void*)s.mask_index})
+    if (!aligned(p, 4)) return ASYMSPEC_E_ALIGN;
+  const int cus = device_cus();
+  if (cus == 0) return ASYMSPEC_E_DEVICE;
+  // as few parts as give each compute unit four workgroups (what their LDS and
+  // threads let it hold), since each part reads the request's lists again
+  A.T = kShapeMaxTokens;
+  while (A.T > kShapeMinTokens && (long long)s.B * ((s.V + A.T - 1) / A.T) < 4ll * cus) A.T /= 2;
+  A.parts = (s.V + A.T - 1) / A.T;
+  const long long grid = (long long)s.B * A.parts;
+  if (grid > 0x7FFFFFFFll) return ASYMSPEC_E_ARG;
+  const int VE = s.dtype == ASYMSPEC_BF16 ? 8 : 4;
+  const size_t lds = (size_t)A.T * 4 + kShapeMaxDrafts * 4 + 16 + (size_t)A.T / VE * 2;
+  if (s.dtype == ASYMSPEC_BF16) shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, (hipStream_t)stream);
+  else shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, (hipStream_t)stream);
+  return launched();
+}
+
+size_t asymspec_draw_workspace_size(int N, int V, int dtype) {
+  int S;
+  return draw_bytes(N, V, dtype, &S);
+}
+
+int asymspec_draw_tokens(const void* logits, int dtype, int N, int V, int64_t row_stride,
+                         const float* temperature, const float* uniforms, int64_t uniform_stride,
+                         int32_t* token, int64_t token_stride, float* prob, int64_t prob_stride,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  DrawArgs A;
+  const size_t bytes = draw_bytes(N, V, dtype, &A.S);
+  if (bytes == 0) return ASYMSPEC_E_ARG;
+  if (logits == nullptr || temperature == nullptr || token == nullptr || workspace == nullptr) return ASYMSPEC_E_ARG;
+  const int64_t far = 1ll << 40;
+  if (N > 1) {
+    if (row_stride < 0 || row_stride > far) return ASYMSPEC_E_ARG;
+    if (uniforms != nullptr && (uniform_stride < 0 || uniform_stride > far)) return ASYMSPEC_E_ARG;
+    // each row has a place of its own
+    if (token_stride < 1 || token_stride > far) return ASYMSPEC_E_ARG;
+    if (prob != nullptr && (prob_stride < 1 || prob_stride > far)) return ASYMSPEC_E_ARG;
+  }
+  if (!aligned(logits, dtype == ASYMSPEC_BF16 ? 2 : 4) || !aligned(temperature, 4) || !aligned(uniforms, 4) ||
+      !aligned(token, 4) || !aligned(prob, 4) || !aligned(workspace, 16))
+    return ASYMSPEC_E_ALIGN;
+  if (workspace_bytes < bytes) return ASYMSPEC_E_WORKSPACE;
+  if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
+  A.logits = logits;
+  A.row_stride = N > 1 ? row_stride : 0;
+  A.tau = temperature;
+  A.u = uniforms;
+  A.u_stride = uniform_stride;
+  A.token = token;
+  A.token_stride = token_stride;
+  A.prob = prob;
+  A.prob_stride = prob_stride;
+  A.part = (DrawPart*)workspace;
+  A.N = N;
+  A.V = V;
+  hipStream_t st = (hipStream_t)stream;
+  const unsigned grid = (unsigned)N * (unsigned)A.S;
+  if (dtype == ASYMSPEC_BF16) {
+    draw_part_kernel<ASYMSPEC_BF16><<<grid, kDrawThreads, 0, st>>>(A);
+    draw_pick_kernel<ASYMSPEC_BF16><<<N, kDrawThreads, 0, st>>>(A);
+  } else {
+    draw_part_kernel<ASYMSPEC_FP32><<<grid, kDrawThreads, 0, st>>>(A);
+    draw_pick_kernel<ASYMSPEC_FP32><<<N, kDrawThreads, 0, st>>>(A);
+  }
+  return launched();
+}
+
+int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token, const int32_t* draft_tokens,
+                           int64_t draft_stride, int32_t* history, int max_history, const int32_t* lengths,
+                           const int32_t* finished, const int32_t* stop_tokens, int n_stop,
+                           const int32_t* max_lengths, int B, int K, int32_t* lengths_out, int32_t* finished_out,
+                           int32_t* tokens_out, int32_t* counts_out, void* stream) {
+  if (B < 1 || K < 0 || K > 63 || max_history < 1 || n_stop < 0) return ASYMSPEC_E_ARG;
+  if (accept_len == nullptr || next_token == nullptr || history == nullptr || lengths == nullptr ||
+      lengths_out == nullptr || finished_out == nullptr || tokens_out == nullptr || counts_out == nullptr)
+    return ASYMSPEC_E_ARG;
+  if ((K > 0 && draft_tokens == nullptr) || (n_stop > 0 && stop_tokens == nullptr)) return ASYMSPEC_E_ARG;
+  if (K > 0 && B > 1 && (draft_stride < 0 || draft_stride > (1ll << 40))) return ASYMSPEC_E_ARG;
+  for (const void* p : {(const void*)accept_len, (const void*)next_token, (const void*)draft_tokens,
+                        (const void*)history, (const void*)lengths, (const void*)finished, (const void*)stop_tokens,
+                        (const void*)max_lengths, (const void*)lengths_out, (const void*)finished_out,
+                        (const void*)tokens_out, (const void*)counts_out})
+    if (!aligned(p, 4)) return ASYMSPEC_E_ALIGN;
+  if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
+  CommitArgs A;
+  A.accept_len = accept_len; A.next_token = next_token; A.draft_tokens = draft_tokens;
+  A.draft_stride = B > 1 ? draft_stride : 0;
+  A.history = history; A.lengths = lengths; A.finished = finished; A.stop_tokens = stop_tokens;
+  A.max_lengths = max_lengths; A.lengths_out = lengths_out; A.finished_out = finished_out;
+  A.tokens_out = tokens_out; A.counts_out = counts_out;
+  A.max_history = max_history; A.n_stop = n_stop; A.B = B; A.K = K;
+  commit_kernel<<<(unsigned)((B + kCommitPer - 1) / kCommitPer), kCommitThreads, 0, (hipStream_t)stream>>>(A);
+  return launched();
+}
+
+int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const int32_t* release,
+                        int32_t* block_table, int max_blocks, const int32_t* n_blocks, int32_t* free_ring,
+                        int ring_size, const int32_t* free_state, int block_size, int B, int width, int total,
+                        int64_t* slots, int32_t* starts, int32_t* short_out, int32_t* n_blocks_out,
+                        int32_t* free_state_out, void* stream) {
+  if (B < 1 || B > ASYMSPEC_SLOTS_MAX_REQUESTS || block_size < 1 || max_blocks < 1 || ring_size < 1 || width < 0)
+    return ASYMSPEC_E_ARG;
+  if (lengths == nullptr || block_table == nullptr || n_blocks == nullptr || free_ring == nullptr ||
+      free_state == nullptr || slots == nullptr || short_out == nullptr || n_blocks_out == nullptr ||
+      free_state_out == nullptr)
+    return ASYMSPEC_E_ARG;
+  if (width == 0 && (total < 1 || new_tokens == nullptr)) return ASYMSPEC_E_ARG;
+  if ((long long)B * max_blocks > 0x7FFFFFFFll || (long long)B * width > 0x7FFFFFFFll) return ASYMSPEC_E_ARG;
+  // every workgroup reads the state that the call starts from
+  if (n_blocks_out == n_blocks || free_state_out == free_state) return ASYMSPEC_E_ARG;
+  for (const void* p : {(const void*)lengths, (const void*)new_tokens, (const void*)release, (const void*)block_table,
+                        (const void*)n_blocks, (const void*)free_ring, (const void*)free_state, (const void*)starts,
+                        (const void*)short_out, (const void*)n_blocks_out, (const void*)free_state_out})
+    if (!aligned(p, 4)) return ASYMSPEC_E_ALIGN;
+  if (!aligned(slots, 8)) return ASYMSPEC_E_ALIGN;
+  const int cus = device_cus();
+  if (cus == 0) return ASYMSPEC_E_DEVICE;
+  SlotsArgs A;
+  A.lengths = lengths; A.new_tokens = new_tokens; A.release = release; A.table = block_table;
+  A.n_blocks = n_blocks; A.ring = free_ring; A.state = free_state; A.slots = slots; A.starts = starts;
+  A.short_out = short_out; A.n_blocks_out = n_blocks_out; A.state_out = free_state_out;
+  A.max_blocks = max_blocks; A.ring_size = ring_size; A.block_size = block_size;
+  A.B = B; A.width = width; A.total = total;
+  const long long places = width > 0 ? (long long)B * width : total;
+  const long long grid = std::min<long long>((places + kSlotsPerGroup - 1) / kSlotsPerGroup, 4ll * cus);
+  slots_kernel<<<(unsigned)grid, kSlotsThreads, (size_t)(4 * (B + 1)) * 4, (hipStream_t)stream>>>(A);
+  return launched();
+}
+
+}  // extern "C"
