@@ -5,29 +5,37 @@
 // summed, also where a uniform falls next to a step of the distribution: with
 // fp32 weights the steps of a 10^5-token row are uncertain by about as much as
 // the smallest of them is wide.  So the weights and their sums are fp64: steps
-// are then uncertain by 1e-15 of the sum.
+// are then uncertain by 1e-13 of the sum.
 //
-// Two kernels.  draw_part: one workgroup per (row, chunk of 4096 tokens) keeps
-// its chunk in registers, finds its maximum m and sums exp((l - m) / tau).
-// draw_pick: one workgroup per row joins the chunks' sums in their order, finds
-// the chunk that the draw falls into, and reads that chunk again to find the
-// token.
+// Two kernels.  draw_part: one wave per chunk of 1024 tokens keeps its chunk in
+// registers, finds its largest logit m and sums exp((l - m) / tau); no wave
+// waits for another.  draw_pick: one wave per row joins the chunks' sums in
+// their order, finds the chunk that the draw falls into, and reads that chunk
+// again to find the token.  A row is split because the exponentials bound it: one
+// compute unit alone would take about 20 us over 151936 tokens.
+//
+// draw_part runs 19 vector operations a token and about 100 a chunk, 25 a token in
+// all, at 33e12 lane operations a second as this chip issues fp64 ones: 99 us for
+// 512 rows of 256000 bf16 tokens (262 MB, 40 us at a read's rate), 15 us for 128 of
+// 151936.  Chunks of 2048 tokens take 4% less there, but 0.7 us more on one row
+// and in draw_pick; waves that stay and fetch their next chunk ahead take 4% more.
 
 #ifndef ASYMSPEC_STEP_DRAW_H_
 #define ASYMSPEC_STEP_DRAW_H_
 
+#include "../device.h"
 #include "row.h"
 
 namespace asym_step {
 
-constexpr int kDrawThreads = 256;
-constexpr int kDrawPer = 16;                                // tokens of a thread
-constexpr int kDrawChunk = kDrawThreads * kDrawPer;         // tokens of a chunk
+constexpr int kDrawThreads = 256;             // 4 chunks
+constexpr int kDrawPer = 16;                  // tokens of a lane
+constexpr int kDrawChunk = 64 * kDrawPer;     // tokens of a chunk
 
 struct DrawPart {
-  double sum;      // of exp((l - m) / tau) over the chunk
-  float m;         // the chunk's largest logit (-inf: no weight)
-  int32_t arg;     // its first index in the row
+  double sum;      // of exp((l - m) / tau) over the chunk; 0 without any weight
+  float m;         // the chunk's largest logit
+  int32_t arg;     // greedy rows: its first index in the row
 };
 
 struct DrawArgs {
@@ -44,226 +52,225 @@ struct DrawArgs {
   int N, V, S;       // S: chunks of a row
 };
 
-// exp((l - m) / tau) for -inf < l <= m; k = 1 / tau.  Never not a number: below
-// m = +inf, and for any k, an infinite difference has no weight.
-STEP_DEV double draw_weight(float l, float m, double k) {
-  if (l == m) return 1.0;
-  const double d = (double)l - (double)m;
-  return d > -__builtin_huge_val() ? exp(d * k) : 0.0;
-}
+// The weights exp((l - m) / tau) = 2^t, t = k (l - m), of logits l <= m, to 2e-14
+// relative: 2^n times a polynomial in f = t - n, |f| <= 1/2, of degree 9
+// (interpolated at the Chebyshev points of the interval, so near the best of its
+// degree).  n comes out of an addition of 1.5 * 2^52, whose sum holds it in its
+// low word.  A logit of -inf or not a number has weight 0, as has what is below
+// 2^-1074.  Below m = +inf a weight is 1 or 0: flat() turns such logits into ones
+// that give that.
+//
+// The coefficients are kept in scalar registers, where a fused multiply-add reads
+// them in place; as literals each costs two moves (512 rows of 256000 bf16 tokens:
+// 145 us against 121).
+struct DrawScale {
+  double c[10], k, m, least;
+  bool inf;
+  STEP_DEV DrawScale(float tau, float top)
+      : c{0x1.000000000003dp+0,  0x1.62e42fefa39f7p-1,  0x1.ebfbdff8149f2p-3,  0x1.c6b08d7044119p-5,
+          0x1.3b2ab72b175eep-7,  0x1.5d87fe908f88ap-10, 0x1.43088e257f341p-13, 0x1.ffcb76789860fp-17,
+          0x1.63ef969a64d3cp-20, 0x1.b6571de2f2351p-24} {
+#pragma unroll
+    for (int i = 0; i < 9; ++i) asm("" : "+s"(c[i]));
+    asm("" : "+v"(c[9]));      // (an instruction reads one scalar at most)
+    // (an infinite temperature is a very large one: it leaves -inf without weight)
+    const double t = __builtin_fmin((double)tau, 0x1p200);
+    double r = __builtin_amdgcn_rcp(t);       // and two steps of Newton's method
+    r = __builtin_fma(r, __builtin_fma(-t, r, 1.0), r);
+    r = __builtin_fma(r, __builtin_fma(-t, r, 1.0), r);
+    k = 1.4426950408889634074 * r;
+    inf = top == __builtin_huge_valf();
+    m = inf ? 0.0 : (double)top;
+    least = -762.0 * t;        // 2^-1099
+  }
+  STEP_DEV float flat(float l) const { return l == __builtin_huge_valf() ? 0.0f : -__builtin_huge_valf(); }
+  // (of a logit that went through flat() where inf)
+  STEP_DEV double weight(double l) const {
+    const double d = __builtin_fmax(l - m, least);
+    const double s = __builtin_fma(k, d, 0x1.8p52), n = s - 0x1.8p52;
+    const double f = __builtin_fma(k, d, -n);
+    double p = __builtin_fma(c[9], f, c[8]);
+#pragma unroll
+    for (int i = 7; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
+    return __builtin_ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, s));
+  }
+};
 
-// Tokens x0 .. x0 + kDrawPer - 1 of a row as fp32; past its end, and where it
-// is not a number, -inf.
+// A lane's 16 tokens of the chunk at x0 of a row: vectors first, first + step, ...
+// of the chunk.  Past the row's end -inf.
 template <int DT>
-STEP_DEV void draw_load(const typename Row<DT>::T* row, int x0, int V, float* l) {
-  constexpr int VE = Row<DT>::VE;
-  if (x0 + kDrawPer <= V) {
-    u4 v[kDrawPer / VE];
+STEP_DEV void draw_load(const typename Row<DT>::T* row, int x0, int V, int first, int step,
+                        u4 (&v)[kDrawPer / Row<DT>::VE]) {
+  constexpr int VE = Row<DT>::VE, NV = kDrawPer / VE;
+  if (x0 + kDrawChunk <= V) {       // the same for the whole wave: nothing between the loads
 #pragma unroll
-    for (int i = 0; i < kDrawPer / VE; ++i) v[i] = load_vec<DT>(row + x0 + i * VE);
-#pragma unroll
-    for (int i = 0; i < kDrawPer; ++i) l[i] = Row<DT>::get(v[i / VE], i % VE);
+    for (int i = 0; i < NV; ++i) v[i] = load_vec<DT>(row + x0 + (first + i * step) * VE);
   } else {
 #pragma unroll
-    for (int i = 0; i < kDrawPer; ++i) l[i] = x0 + i < V ? Row<DT>::get1(row[x0 + i]) : -__builtin_huge_valf();
-  }
+    for (int i = 0; i < NV; ++i) {
+      v[i] = Row<DT>::neg_inf();
+      const int x = x0 + (first + i * step) * VE;
 #pragma unroll
-  for (int i = 0; i < kDrawPer; ++i)
-    if (l[i] != l[i]) l[i] = -__builtin_huge_valf();
-}
-
-// The larger logit, and of two equal ones the lower index.
-STEP_DEV void draw_max(float& m, int& arg, float m2, int arg2) {
-  if (m2 > m || (m2 == m && arg2 < arg)) {
-    m = m2;
-    arg = arg2;
+      for (int e = 0; e < VE; ++e)
+        if (x + e < V) Row<DT>::put_bits(v[i], e, row[x + e]);
+    }
   }
+}
+template <int DT>
+STEP_DEV void draw_decode(const u4 (&v)[kDrawPer / Row<DT>::VE], float (&l)[kDrawPer]) {
+  constexpr int VE = Row<DT>::VE;
+#pragma unroll
+  for (int i = 0; i < kDrawPer; ++i) l[i] = Row<DT>::get(v[i / VE], i % VE);
 }
 
 template <int DT>
 __global__ __launch_bounds__(kDrawThreads) void draw_part_kernel(DrawArgs A) {
-  __shared__ float sm[kDrawThreads / 64];
-  __shared__ int sa[kDrawThreads / 64];
-  __shared__ double ss[kDrawThreads / 64];
-  const int tid = (int)threadIdx.x, wave = tid >> 6;
-  const int row = (int)(blockIdx.x / (unsigned)A.S), s = (int)(blockIdx.x % (unsigned)A.S);
-  const typename Row<DT>::T* p = (const typename Row<DT>::T*)A.logits + row * A.row_stride;
-  const int x0 = s * kDrawChunk + tid * kDrawPer;
-  float l[kDrawPer];
-  draw_load<DT>(p, x0, A.V, l);
-  float m = l[0];
-  int arg = x0;
-#pragma unroll
-  for (int i = 1; i < kDrawPer; ++i)
-    if (l[i] > m) {
-      m = l[i];
-      arg = x0 + i;
-    }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) draw_max(m, arg, __shfl_xor(m, off, 64), __shfl_xor(arg, off, 64));
-  if ((tid & 63) == 0) {
-    sm[wave] = m;
-    sa[wave] = arg;
-  }
-  __syncthreads();
-  m = sm[0];
-  arg = sa[0];
-#pragma unroll
-  for (int w = 1; w < kDrawThreads / 64; ++w) draw_max(m, arg, sm[w], sa[w]);
+  constexpr int VE = Row<DT>::VE;
+  const int lane = (int)threadIdx.x & 63;
+  const unsigned id = blockIdx.x * (kDrawThreads / 64) + (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const unsigned row = id / (unsigned)A.S;
+  if (row >= (unsigned)A.N) return;
+  const int x0 = (int)(id - row * (unsigned)A.S) * kDrawChunk;
   const float tau = A.tau[row];
+  u4 v[kDrawPer / VE];
+  draw_load<DT>((const typename Row<DT>::T*)A.logits + row * A.row_stride, x0, A.V, lane, 64, v);
+  float l[kDrawPer];
+  draw_decode<DT>(v, l);
+  // The maximum as fp64, which the weights need too: the conversion makes every
+  // not-a-number a quiet one, which fmax leaves out.
+  double top = -__builtin_huge_val();
+#pragma unroll
+  for (int i = 0; i < kDrawPer; ++i) top = __builtin_fmax(top, (double)l[i]);
+  const float m = asym::wave_max((float)top);
   double sum = 0.0;
-  if (tau > 0.0f && m > -__builtin_huge_valf()) {
-    const double k = 1.0 / (double)tau;
+  int arg = 0;
+  if (!(tau > 0.0f)) {
+    arg = 0x7FFFFFFF;
 #pragma unroll
-    for (int i = 0; i < kDrawPer; ++i)
-      if (l[i] > -__builtin_huge_valf()) sum += draw_weight(l[i], m, k);
+    for (int i = kDrawPer - 1; i >= 0; --i)
+      if (l[i] == m) arg = x0 + ((i / VE) * 64 + lane) * VE + i % VE;
+    arg = asym::wave_min_i(arg);
+  } else if (m > -__builtin_huge_valf()) {
+    const DrawScale k(tau, m);
+    if (k.inf) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    if ((tid & 63) == 0) ss[wave] = sum;
-    __syncthreads();
-    sum = 0.0;
+      for (int i = 0; i < kDrawPer; ++i) l[i] = k.flat(l[i]);
+    }
+    double part[2] = {0.0, 0.0};
 #pragma unroll
-    for (int w = 0; w < kDrawThreads / 64; ++w) sum += ss[w];
+    for (int i = 0; i < kDrawPer; ++i) part[i & 1] += k.weight((double)l[i]);
+    double before;
+    asym::wave_scan_d(part[0] + part[1], sum, before);
   }
-  if (tid == 0) A.part[(size_t)row * A.S + s] = DrawPart{sum, m, arg};
-}
-
-// Inclusive sums over the workgroup's threads, in their order.
-STEP_DEV double draw_scan(double v, double* lds, double& total) {
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
-  __syncthreads();
-  if (lane == 63) lds[wave] = v;
-  __syncthreads();
-  double before = 0.0;
-  total = 0.0;
-#pragma unroll
-  for (int w = 0; w < kDrawThreads / 64; ++w) {
-    if (w < wave) before += lds[w];
-    total += lds[w];
-  }
-  return before + v;
+  if (lane == 63) A.part[id] = DrawPart{sum, m, arg};
 }
 
 template <int DT>
-__global__ __launch_bounds__(kDrawThreads) void draw_pick_kernel(DrawArgs A) {
-  __shared__ float sm[kDrawThreads / 64];
-  __shared__ int sa[kDrawThreads / 64];
-  __shared__ double lds[kDrawThreads / 64];
-  __shared__ int found, last;
-  __shared__ double found_before;
-  const int tid = (int)threadIdx.x, row = (int)blockIdx.x;
+__global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
+  constexpr int VE = Row<DT>::VE;
+  const int lane = (int)threadIdx.x, row = (int)blockIdx.x;
   const DrawPart* P = A.part + (size_t)row * A.S;
   const float inf = __builtin_huge_valf();
-  // the row's largest logit
-  float m = -inf;
-  int arg = 0x7FFFFFFF;
-  for (int s = tid; s < A.S; s += kDrawThreads) draw_max(m, arg, P[s].m, P[s].arg);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) draw_max(m, arg, __shfl_xor(m, off, 64), __shfl_xor(arg, off, 64));
-  if ((tid & 63) == 0) {
-    sm[tid >> 6] = m;
-    sa[tid >> 6] = arg;
-  }
-  if (tid == 0) {
-    found = 0x7FFFFFFF;
-    last = -1;
-  }
-  __syncthreads();
-  m = sm[0];
-  arg = sa[0];
-#pragma unroll
-  for (int w = 1; w < kDrawThreads / 64; ++w) draw_max(m, arg, sm[w], sa[w]);
+  const float tau = A.tau[row];
+  float u = A.u ? A.u[row * A.u_stride] : 0.0f;
+  if (!(u > 0.0f)) u = 0.0f;
   int32_t* token = A.token + row * A.token_stride;
   float* prob = A.prob ? A.prob + row * A.prob_stride : nullptr;
-  const float tau = A.tau[row];
+
+  // The chunk that the draw falls into: each lane has a run of chunks.
+  const int per = (A.S + 63) / 64;
+  const int lo = min(A.S, lane * per), hi = min(A.S, lo + per);
+  float mine_m = -inf;
+  int arg = 0x7FFFFFFF;
+  for (int s = lo; s < hi; ++s) {
+    const float x = P[s].m;
+    if (x > mine_m) {
+      mine_m = x;
+      arg = P[s].arg;
+    }
+  }
+  const float m = asym::wave_max(mine_m);
   if (!(tau > 0.0f) || m == -inf) {
-    if (tid == 0) {
+    arg = asym::wave_min_i(mine_m == m ? arg : 0x7FFFFFFF);
+    if (lane == 0) {
       *token = m == -inf ? 0 : arg;
       if (prob) *prob = m == -inf ? 0.0f : 1.0f;
     }
     return;
   }
-  const double k = 1.0 / (double)tau;
-  // the chunk that the draw falls into: each thread has a run of chunks
-  const int per = (A.S + kDrawThreads - 1) / kDrawThreads;
-  const int lo = min(A.S, tid * per), hi = min(A.S, lo + per);
-  auto chunk_sum = [&](int s) { return P[s].m > -inf ? P[s].sum * draw_weight(P[s].m, m, k) : 0.0; };
-  double mine = 0.0;
-  for (int s = lo; s < hi; ++s) mine += chunk_sum(s);
-  double total;
-  const double upto = draw_scan(mine, lds, total);
-  float u = A.u ? A.u[row * A.u_stride] : 0.0f;
-  if (!(u > 0.0f)) u = 0.0f;
+  const DrawScale k(tau, m);
+  auto chunk = [&](int s) {
+    const DrawPart q = P[s];
+    return q.sum * k.weight((double)(k.inf ? k.flat(q.m) : q.m));
+  };
+  double mine = 0.0, upto, ahead;
+  for (int s = lo; s < hi; ++s) mine += chunk(s);
+  asym::wave_scan_d(mine, upto, ahead);
+  const double total = __shfl(upto, 63, 64);
   const double target = (double)u * total;
-  {
-    double c = upto - mine;
-    int f = -1, z = -1;
-    double fb = 0.0;
+  // the first lane whose sums pass the target; without one (a uniform of 1) the
+  // last lane with weight
+  const unsigned long long past = __ballot(upto > target && mine > 0.0), some = __ballot(mine > 0.0);
+  const bool none = past == 0ull;
+  const int from = none ? 63 - __clzll((long long)(some | 1ull)) : __ffsll(past) - 1;
+  int at = lo;
+  double before = ahead;
+  if (per > 1) {
+    double c = ahead;
+    bool found = false;
     for (int s = lo; s < hi; ++s) {
-      const double w = chunk_sum(s);
-      if (w > 0.0) z = s;
-      if (f < 0 && c + w > target && w > 0.0) {
-        f = s;
-        fb = c;
+      const double w = chunk(s);
+      if (w > 0.0 && !found) {
+        at = s;
+        before = c;
+        found = !none && c + w > target;
       }
       c += w;
     }
-    if (f >= 0) atomicMin(&found, f);
-    if (z >= 0) atomicMax(&last, z);
-    __syncthreads();
-    if (f >= 0 && found == f) found_before = fb;
-    // no sum exceeds the target: the last token with weight
-    const bool none = found == 0x7FFFFFFF;
-    __syncthreads();
-    if (none && tid == 0) {
-      found = last;
-      found_before = -__builtin_huge_val();
-    }
-    __syncthreads();
   }
-  const int s = max(found, 0);      // (the chunk of the largest logit has weight, so one was found)
-  const double before = found_before;
-  __syncthreads();
-  if (tid == 0) {
-    found = 0x7FFFFFFF;
-    last = -1;
-  }
+  at = __shfl(at, from, 64);
+  before = __shfl(before, from, 64);
+
+  // The token in it: each lane has 16 consecutive ones.  The first lane whose
+  // sums pass the target holds it; if rounding, or a uniform of 1, puts the target
+  // behind all of them, the last lane with weight, and its last such token.
   const typename Row<DT>::T* p = (const typename Row<DT>::T*)A.logits + row * A.row_stride;
-  const int x0 = s * kDrawChunk + tid * kDrawPer;
+  const int x0 = at * kDrawChunk + lane * kDrawPer;
+  u4 v[kDrawPer / VE];
+  draw_load<DT>(p, at * kDrawChunk, A.V, lane * (kDrawPer / VE), 1, v);
   float l[kDrawPer];
-  draw_load<DT>(p, x0, A.V, l);
+  draw_decode<DT>(v, l);
+  if (k.inf) {
+#pragma unroll
+    for (int i = 0; i < kDrawPer; ++i) l[i] = k.flat(l[i]);
+  }
   double w[kDrawPer];
-  mine = 0.0;
+  double sum = 0.0, incl, excl;
 #pragma unroll
   for (int i = 0; i < kDrawPer; ++i) {
-    w[i] = l[i] > -inf ? draw_weight(l[i], m, k) : 0.0;
-    mine += w[i];
+    w[i] = k.weight((double)l[i]);
+    sum += w[i];
   }
-  double unused;
-  const double up = draw_scan(mine, lds, unused);
-  double c = before + (up - mine);
-  int f = -1, z = -1;
+  asym::wave_scan_d(sum, incl, excl);
+  const unsigned long long over = none ? 0ull : __ballot(before + incl > target && sum > 0.0);
+  const unsigned long long has = __ballot(sum > 0.0);
+  const int who = over != 0ull ? __ffsll(over) - 1 : 63 - __clzll((long long)(has | 1ull));
+  if (lane == who) {
+    double c = before + excl, wt = 0.0;
+    int t = 0;
+    bool found = false;
 #pragma unroll
-  for (int i = 0; i < kDrawPer; ++i) {
-    c += w[i];
-    if (w[i] > 0.0) z = x0 + i;
-    if (f < 0 && w[i] > 0.0 && c > target) f = x0 + i;
-  }
-  if (f >= 0) atomicMin(&found, f);
-  if (z >= 0) atomicMax(&last, z);
-  __syncthreads();
-  const int t = found != 0x7FFFFFFF ? found : last;
-#pragma unroll
-  for (int i = 0; i < kDrawPer; ++i)
-    if (x0 + i == t) {
-      *token = t;
-      if (prob) *prob = (float)(w[i] / total);
+    for (int i = 0; i < kDrawPer; ++i) {
+      if (w[i] > 0.0 && !found) {
+        t = x0 + i;
+        wt = w[i];
+        found = over != 0ull && c + w[i] > target;
+      }
+      c += w[i];
     }
+    *token = t;
+    if (prob) *prob = (float)(wt / total);
+  }
 }
 
 }  // namespace asym_step

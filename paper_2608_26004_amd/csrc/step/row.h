@@ -36,9 +36,10 @@ template <> struct Row<ASYMSPEC_BF16> {
     if ((u & 0x7FFFFFFFu) > kInfBits) return (u >> 16) | 0x40u;
     return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
   }
-  static STEP_DEV void put(u4& v, int e, float f) {
-    v[e >> 1] = (e & 1) ? ((v[e >> 1] & 0xFFFFu) | (bits(f) << 16)) : ((v[e >> 1] & 0xFFFF0000u) | bits(f));
+  static STEP_DEV void put_bits(u4& v, int e, uint32_t b) {
+    v[e >> 1] = (e & 1) ? ((v[e >> 1] & 0xFFFFu) | (b << 16)) : ((v[e >> 1] & 0xFFFF0000u) | b);
   }
+  static STEP_DEV void put(u4& v, int e, float f) { put_bits(v, e, bits(f)); }
   static STEP_DEV u4 neg_inf() { return u4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
   static STEP_DEV float get1(T b) { return __uint_as_float((uint32_t)b << 16); }
   static STEP_DEV T put1(float f) { return (T)bits(f); }
@@ -49,6 +50,7 @@ template <> struct Row<ASYMSPEC_FP32> {
   typedef uint32_t T;
   typedef uint32_t U __attribute__((ext_vector_type(4), aligned(4)));
   static STEP_DEV float get(const u4& v, int e) { return __uint_as_float(v[e]); }
+  static STEP_DEV void put_bits(u4& v, int e, uint32_t b) { v[e] = b; }
   static STEP_DEV void put(u4& v, int e, float f) { v[e] = __float_as_uint(f); }
   static STEP_DEV u4 neg_inf() { return u4{kNegInfBits, kNegInfBits, kNegInfBits, kNegInfBits}; }
   static STEP_DEV float get1(T b) { return __uint_as_float(b); }

@@ -172,13 +172,13 @@ int asymspec_draw_tokens(const void* logits, int dtype, int N, int V, int64_t ro
   A.N = N;
   A.V = V;
   hipStream_t st = (hipStream_t)stream;
-  const unsigned grid = (unsigned)N * (unsigned)A.S;
+  const unsigned grid = (unsigned)(((long long)N * A.S + kDrawThreads / 64 - 1) / (kDrawThreads / 64));
   if (dtype == ASYMSPEC_BF16) {
     draw_part_kernel<ASYMSPEC_BF16><<<grid, kDrawThreads, 0, st>>>(A);
-    draw_pick_kernel<ASYMSPEC_BF16><<<N, kDrawThreads, 0, st>>>(A);
+    draw_pick_kernel<ASYMSPEC_BF16><<<N, 64, 0, st>>>(A);
   } else {
     draw_part_kernel<ASYMSPEC_FP32><<<grid, kDrawThreads, 0, st>>>(A);
-    draw_pick_kernel<ASYMSPEC_FP32><<<N, kDrawThreads, 0, st>>>(A);
+    draw_pick_kernel<ASYMSPEC_FP32><<<N, 64, 0, st>>>(A);
   }
   return launched();
 }

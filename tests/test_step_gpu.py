@@ -250,6 +250,17 @@ def test_draw_special_rows():
     assert tok[12] == 7999 and tok[13] == V - 1 and tok[14] == 3 and tok[15] == 0
 
 
+def test_draw_every_kind_of_not_a_number():
+    """Quiet and signalling ones of either sign, as bf16 bit patterns."""
+    V = 5000
+    bits = np.full((2, V), 0x3F80, np.uint16)                  # 1.0
+    bits[:, 0::4], bits[:, 1::4], bits[:, 2::4] = 0x7F81, 0x7FC0, 0xFF81
+    x = gpu(bits.view(np.int16)).view(torch.bfloat16)
+    tok, q = asp.draw_tokens(x, gpu(np.float32([0, 1])), gpu(np.float32([0.5, 0.5])))
+    assert tok[0] == 3 and q[0] == 1.0
+    assert tok[1] == 4 * 625 + 3 and q[1].item() == np.float32(1 / 1250)
+
+
 def test_draw_strided_views_and_out():
     """One position of the rows' buffer in, columns of [B][K] buffers out; the
     other columns stay; the same bits with a workspace and without, twice."""
