@@ -258,5 +258,14 @@ def fuse_verify(t, a, b, draft_tokens, draft_probs, uniforms, temperature,
     return res
 
 
-# the operators around the decision step
-from .step import commit_tokens, draw_tokens, plan_slots, shape_logits  # noqa: E402
+# the operators around the decision step (step.py), loaded at their first use
+_STEP = ("shape_logits", "draw_tokens", "commit_tokens", "plan_slots")
+
+
+def __getattr__(name):
+    if name in _STEP:
+        from . import step
+        for n in _STEP:
+            globals()[n] = getattr(step, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

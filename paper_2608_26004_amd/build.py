@@ -108,6 +108,34 @@ def build_example(verbose: bool = False) -> str:
     return EXAMPLE
 
 
+BIND_SRC = os.path.join(CSRC, "step", "bind.cpp")
+BIND = os.path.join(HERE, "_step.so")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """_step.so: the Python binding of the operators around the decision step,
+    host code against torch's C++ interface, linked to libasymspec.so."""
+    import sysconfig
+
+    import torch
+    at = os.path.join(os.path.dirname(os.path.abspath(torch.__file__)))
+    tmp = BIND + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", os.path.join(at, "include"),
+           "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include", "-I", INC, BIND_SRC,
+           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
+           "-L", HERE, "-lasymspec", "-L", "/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,$ORIGIN", "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"binding build failed ({r.returncode}):\n{r.stdout}{r.stderr}")
+    os.replace(tmp, BIND)
+    if verbose:
+        print(f"built {BIND}")
+    return BIND
+
+
 PROBE_SRC = os.path.join(HERE, "csrc", "probe.hip")
 PROBE = os.path.join(HERE, "libasymspec_probe.so")
 
@@ -127,6 +155,7 @@ def build_probe(verbose: bool = False) -> str:
 
 if __name__ == "__main__":
     print(build(verbose=True))
+    build_binding(verbose=True)
     build_example(verbose=True)
     build_probe(verbose=True)
     sys.exit(0)

@@ -10,12 +10,34 @@ import pytest
 import torch
 
 import paper_2608_26004_amd as asp
-from paper_2608_26004_amd import step
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "asymspec_step.h")
 FAKE = 1 << 20
 ODD = FAKE + 2
+VP, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+
+
+class Shape(ctypes.Structure):
+    """asymspec_shape."""
+    _fields_ = ([(n, VP) for n in ("logits", "out")]
+                + [(n, I64) for n in ("request_stride", "row_stride", "out_request_stride", "out_row_stride")]
+                + [(n, VP) for n in ("history", "lengths", "prompt_lengths", "draft_tokens")] + [("draft_stride", I64)]
+                + [(n, VP) for n in ("id_map", "repetition", "frequency", "presence", "bias_ids", "bias_values",
+                                     "mask", "mask_index")]
+                + [(n, ctypes.c_int32) for n in ("dtype", "B", "R", "V", "max_history", "D", "n_ids", "n_bias",
+                                                 "n_masks")])
+
+
+def library():
+    lib = asp.load_library()
+    lib.asymspec_shape_logits.argtypes = [ctypes.POINTER(Shape), VP]
+    lib.asymspec_draw_workspace_size.argtypes = [I32, I32, I32]
+    lib.asymspec_draw_workspace_size.restype = SZ
+    lib.asymspec_draw_tokens.argtypes = [VP, I32, I32, I32, I64, VP, VP, I64, VP, I64, VP, I64, VP, SZ, VP]
+    lib.asymspec_commit_tokens.argtypes = [VP, VP, VP, I64, VP, I32, VP, VP, VP, I32, VP, I32, I32, VP, VP, VP, VP, VP]
+    lib.asymspec_plan_slots.argtypes = [VP, VP, VP, VP, I32, VP, VP, I32, VP, I32, I32, I32, I32, VP, VP, VP, VP, VP, VP]
+    return lib
 
 
 def test_library_exports_header_symbols():
@@ -23,7 +45,7 @@ def test_library_exports_header_symbols():
     names = sorted(set(re.findall(r"\b(asymspec_[a-z_]+)\s*\(", src)))
     assert len(names) == 5
     for n in names:
-        assert hasattr(step._library(), n), n
+        assert hasattr(library(), n), n
 
 
 def test_struct_layout_matches_header():
@@ -31,7 +53,7 @@ def test_struct_layout_matches_header():
     src = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     body = re.search(r"typedef struct asymspec_shape \{(.*?)\} asymspec_shape;", src, re.S).group(1)
     names = re.findall(r"\*?\s*(\w+)\s*[,;]", body)
-    assert names == [f[0] for f in step._Shape._fields_]
+    assert names == [f[0] for f in Shape._fields_]
 
 
 def shape_call(**over):
@@ -40,7 +62,7 @@ def shape_call(**over):
               repetition=FAKE, frequency=FAKE, presence=FAKE, bias_ids=FAKE, bias_values=FAKE, mask=FAKE,
               mask_index=FAKE, dtype=asp.FP32, B=4, R=3, V=100, max_history=50, D=2, n_ids=0, n_bias=5, n_masks=7)
     kw.update(over)
-    return step._library().asymspec_shape_logits(ctypes.byref(step._Shape(**kw)), None)
+    return library().asymspec_shape_logits(ctypes.byref(Shape(**kw)), None)
 
 
 @pytest.mark.parametrize("over,code", [
@@ -86,7 +108,7 @@ def draw_call(**over):
     kw = dict(logits=FAKE, dtype=asp.BF16, N=3, V=5000, stride=5000, tau=FAKE, u=FAKE, us=1, token=FAKE, ts=1,
               prob=FAKE, ps=1, ws=FAKE, wsb=1 << 20)
     kw.update(over)
-    return step._library().asymspec_draw_tokens(*kw.values(), None)
+    return library().asymspec_draw_tokens(*kw.values(), None)
 
 
 @pytest.mark.parametrize("over,code", [
@@ -102,7 +124,7 @@ def test_draw_refusals(over, code):
 
 
 def test_draw_workspace_size():
-    size = step._library().asymspec_draw_workspace_size
+    size = library().asymspec_draw_workspace_size
     assert size(1, 1, asp.FP32) > 0 and size(4, 100000, asp.BF16) == 4 * size(1, 100000, asp.BF16)
     for bad in ((0, 5, 0), (1, 0, 0), (1, 1 << 30, 0), (1, 5, 2), (-1, 5, 0)):
         assert size(*bad) == 0
@@ -112,7 +134,7 @@ def commit_call(**over):
     kw = dict(acc=FAKE, nxt=FAKE, d=FAKE, ds=2, hist=FAKE, L=100, lens=FAKE, fin=FAKE, stops=FAKE, n_stop=2,
               maxl=FAKE, B=3, K=2, lo=FAKE, fo=FAKE, to=FAKE, co=FAKE)
     kw.update(over)
-    return step._library().asymspec_commit_tokens(*kw.values(), None)
+    return library().asymspec_commit_tokens(*kw.values(), None)
 
 
 @pytest.mark.parametrize("over,code", [
@@ -130,7 +152,7 @@ def slots_call(**over):
     kw = dict(lens=FAKE, new=FAKE, rel=FAKE, table=FAKE, top=10, held=FAKE, ring=FAKE, N=100, state=FAKE, bs=16, B=3,
               width=2, total=0, slots=FAKE, starts=FAKE, short=FAKE, held_out=FAKE * 2, state_out=FAKE * 2)
     kw.update(over)
-    return step._library().asymspec_plan_slots(*kw.values(), None)
+    return library().asymspec_plan_slots(*kw.values(), None)
 
 
 @pytest.mark.parametrize("over,code", [
