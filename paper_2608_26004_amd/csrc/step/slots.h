@@ -16,7 +16,6 @@
 namespace asym_step {
 
 constexpr int kSlotsThreads = 256;
-constexpr int kSlotsPerGroup = 1024;      // list entries of a workgroup
 
 struct SlotsArgs {
   const int32_t* lengths;
@@ -34,20 +33,22 @@ struct SlotsArgs {
   int max_blocks, ring_size, block_size, B, width, total;
 };
 
-// What a request has and needs.
+// What a request has and needs.  Lengths and new tokens are below 2^31 each, so
+// positions fit 32 bits without a sign.
 struct SlotsReq {
-  int64_t need;
+  uint32_t need;          // blocks
   int held, fresh;        // blocks held; new tokens
 };
 STEP_DEV SlotsReq slots_req(const SlotsArgs& A, int b) {
-  SlotsReq q;
+  const int given = A.new_tokens ? A.new_tokens[b] : A.width, len = A.lengths[b], held = A.n_blocks[b];
   const bool gone = A.release && A.release[b] != 0;
-  int n = A.new_tokens ? max(A.new_tokens[b], 0) : A.width;
+  int n = max(given, 0);
   if (A.width > 0) n = min(n, A.width);
+  const uint32_t end = (uint32_t)max(len, 0) + (uint32_t)n, bs = (uint32_t)A.block_size, full = end / bs;
+  SlotsReq q;
   q.fresh = gone ? 0 : n;
-  const int64_t len = max(A.lengths[b], 0);
-  q.need = gone ? 0 : (len + n + A.block_size - 1) / A.block_size;
-  q.held = min(max(A.n_blocks[b], 0), A.max_blocks);
+  q.need = gone ? 0u : full + (end != full * bs ? 1u : 0u);
+  q.held = min(max(held, 0), A.max_blocks);
   return q;
 }
 
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(kSlotsThreads) void slots_kernel(SlotsArgs A) {
   int64_t v[3] = {0, 0, 0};
   for (int b = lo; b < hi; ++b) {
     const SlotsReq q = slots_req(A, b);
-    delta[b] = q.need <= A.max_blocks ? (int)q.need - q.held : kShort;
+    delta[b] = q.need <= (uint32_t)A.max_blocks ? (int)q.need - q.held : kShort;
     start[b] = q.fresh;
     if (delta[b] > 0) v[0] += delta[b];
   }
@@ -151,29 +152,30 @@ __global__ __launch_bounds__(kSlotsThreads) void slots_kernel(SlotsArgs A) {
   auto held_of = [&](int b) { return min(max(A.n_blocks[b], 0), A.max_blocks); };
   const int first = (int)blockIdx.x * kSlotsThreads + tid, step = (int)gridDim.x * kSlotsThreads;
 
-  const int n_taken = taken[B], n_given = given[B];
-  for (int64_t i = first; i < n_taken; i += step) {
-    const int b = slots_find(taken, B, (int)i);
-    A.table[(size_t)b * A.max_blocks + held_of(b) + ((int)i - taken[b])] = *ring_at((int)i);
-  }
-  for (int64_t i = first; i < n_given; i += step) {
-    const int b = slots_find(given, B, (int)i);
-    int32_t* e = A.table + (size_t)b * A.max_blocks + held_of(b) + delta[b] + ((int)i - given[b]);
-    if (i < N - count) *ring_at(count + (int)i) = *e;
-    *e = -1;
-  }
-  const int places = A.width > 0 ? B * A.width : A.total;
-  for (int64_t i = first; i < places; i += step) {
-    const int b = A.width > 0 ? (int)i / A.width : slots_find(start, B, (int)i);
-    const int j = A.width > 0 ? (int)i - b * A.width : (int)i - start[b];
-    int64_t slot = -1;
-    if (j < start[b + 1] - start[b] && delta[b] != kShort) {
-      const int64_t p = (int64_t)max(A.lengths[b], 0) + j;
-      const int k = (int)(p / A.block_size), held = held_of(b);
-      const int id = k < held ? A.table[(size_t)b * A.max_blocks + k] : *ring_at(taken[b] + (k - held));
-      slot = (int64_t)id * A.block_size + (p - (int64_t)k * A.block_size);
+  // the lists one behind the other, so that a thread has few entries of any
+  const int places = A.width > 0 ? B * A.width : A.total, n_taken = taken[B], n_given = given[B];
+  const int64_t all = (int64_t)places + n_taken + n_given;
+  for (int64_t i = first; i < all; i += step) {
+    if (i < places) {
+      const int b = A.width > 0 ? (int)((uint32_t)i / (uint32_t)A.width) : slots_find(start, B, (int)i);
+      const int j = A.width > 0 ? (int)i - b * A.width : (int)i - start[b];
+      int64_t slot = -1;
+      if (j < start[b + 1] - start[b] && delta[b] != kShort) {
+        const uint32_t p = (uint32_t)max(A.lengths[b], 0) + (uint32_t)j, bs = (uint32_t)A.block_size;
+        const int k = (int)(p / bs), held = held_of(b);
+        const int id = k < held ? A.table[(size_t)b * A.max_blocks + k] : *ring_at(taken[b] + (k - held));
+        slot = (int64_t)id * A.block_size + (p - (uint32_t)k * bs);
+      }
+      A.slots[i] = slot;
+    } else if (i < (int64_t)places + n_taken) {
+      const int q = (int)(i - places), b = slots_find(taken, B, q);
+      A.table[(size_t)b * A.max_blocks + held_of(b) + (q - taken[b])] = *ring_at(q);
+    } else {
+      const int q = (int)(i - places - n_taken), b = slots_find(given, B, q);
+      int32_t* e = A.table + (size_t)b * A.max_blocks + held_of(b) + delta[b] + (q - given[b]);
+      if (q < N - count) *ring_at(count + q) = *e;
+      *e = -1;
     }
-    A.slots[i] = slot;
   }
   for (int b = first; b < B; b += step) {
     const bool is_short = delta[b] == kShort;

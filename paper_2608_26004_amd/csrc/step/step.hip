@@ -240,7 +240,11 @@ int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const
   A.max_blocks = max_blocks; A.ring_size = ring_size; A.block_size = block_size;
   A.B = B; A.width = width; A.total = total;
   const long long places = width > 0 ? (long long)B * width : total;
-  const long long grid = std::min<long long>((places + kSlotsPerGroup - 1) / kSlotsPerGroup, 4ll * cus);
+  // An entry a thread, up to two workgroups per compute unit: the slots, the blocks
+  // taken (an eighth of them is plenty) and those given back, which the host does
+  // not know: a request that ends gives all it has, so one table in 32.
+  const long long entries = places + places / 8 + (long long)B * max_blocks / 32;
+  const long long grid = std::min<long long>(entries / kSlotsThreads + 1, 2ll * cus);
   slots_kernel<<<(unsigned)grid, kSlotsThreads, (size_t)(4 * (B + 1)) * 4, (hipStream_t)stream>>>(A);
   return launched();
 }
