@@ -41,6 +41,16 @@ template <> struct Row<ASYMSPEC_BF16> {
   }
   static STEP_DEV void put(u4& v, int e, float f) { put_bits(v, e, bits(f)); }
   static STEP_DEV u4 neg_inf() { return u4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}; }
+  // -inf in place of each token e whose bit of `allowed` is clear
+  static STEP_DEV void mask(u4& v, uint32_t allowed) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = 0u - ((allowed >> (2 * i)) & 1u), hi = 0u - ((allowed >> (2 * i + 1)) & 1u);
+      const uint32_t keep = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+      v[i] = (v[i] & keep) | (0xFF80FF80u & ~keep);
+    }
+  }
+  static STEP_DEV T elem(const u4& v, int e) { return (T)(v[e >> 1] >> (16 * (e & 1))); }
   static STEP_DEV float get1(T b) { return __uint_as_float((uint32_t)b << 16); }
   static STEP_DEV T put1(float f) { return (T)bits(f); }
 };
@@ -53,6 +63,11 @@ template <> struct Row<ASYMSPEC_FP32> {
   static STEP_DEV void put_bits(u4& v, int e, uint32_t b) { v[e] = b; }
   static STEP_DEV void put(u4& v, int e, float f) { v[e] = __float_as_uint(f); }
   static STEP_DEV u4 neg_inf() { return u4{kNegInfBits, kNegInfBits, kNegInfBits, kNegInfBits}; }
+  static STEP_DEV void mask(u4& v, uint32_t allowed) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = ((allowed >> i) & 1u) ? v[i] : kNegInfBits;
+  }
+  static STEP_DEV T elem(const u4& v, int e) { return v[e]; }
   static STEP_DEV float get1(T b) { return __uint_as_float(b); }
   static STEP_DEV T put1(float f) { return __float_as_uint(f); }
 };

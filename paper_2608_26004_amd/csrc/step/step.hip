@@ -119,15 +119,20 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
     if (!aligned(p, 4)) return ASYMSPEC_E_ALIGN;
   const int cus = device_cus();
   if (cus == 0) return ASYMSPEC_E_DEVICE;
-  // as few parts as give each compute unit four workgroups (what their LDS and
-  // threads let it hold), since each part reads the request's lists again
-  A.T = kShapeMaxTokens;
-  while (A.T > kShapeMinTokens && (long long)s.B * ((s.V + A.T - 1) / A.T) < 4ll * cus) A.T /= 2;
-  A.parts = (s.V + A.T - 1) / A.T;
+  // The shortest parts that do not make too many workgroups, since each reads the
+  // request's lists again.  In place, as many as are resident at once (four a unit):
+  // 8 x 3 rows of 151936 bf16 tokens behind 4096: 9.2 us at 600 workgroups, 10.4 at
+  // 1192 and 10.0 at 304.  A copy wants about five times as many, so that some copy
+  // while others list: 96 x 6 rows of 50257 fp32 tokens 64 us at 4800 workgroups, 79 at
+  // 672; 64 x 5 rows of 151936 bf16 tokens behind 8192 61 us at 4800, 89 at 9536, 71 at 1216.
+  const long long most = (s.logits == s.out ? 4ll : 20ll) * cus;
+  int T = kShapeMinTokens;
+  while (T < kShapeMaxTokens && (long long)s.B * ((s.V + T - 1) / T) > most) T *= 2;
+  A.lgT = __builtin_ctz((unsigned)T);
+  A.parts = (s.V + T - 1) / T;
   const long long grid = (long long)s.B * A.parts;
   if (grid > 0x7FFFFFFFll) return ASYMSPEC_E_ARG;
-  const int VE = s.dtype == ASYMSPEC_BF16 ? 8 : 4;
-  const size_t lds = (size_t)A.T * 4 + kShapeMaxDrafts * 4 + 16 + (size_t)A.T / VE * 2;
+  const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T) : ShapeLds<4>::bytes(T);
   if (s.dtype == ASYMSPEC_BF16) shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, (hipStream_t)stream);
   else shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, (hipStream_t)stream);
   return launched();

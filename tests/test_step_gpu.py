@@ -142,6 +142,21 @@ def test_shape_untouched_logits_keep_their_bits():
     assert np.array_equal(got[0, 0, same], bits[0, 0, same])
 
 
+def test_shape_rows_ahead_of_a_draft_keep_their_bits():
+    """A token that only stands among the drafts is untouched in the rows ahead of
+    it, whatever its bits, in whole vectors and behind the last one."""
+    V, R = 1029, 3
+    bits = np.full((1, R, V), 0x7F81, np.uint16)               # signalling not-a-numbers
+    x = gpu(bits.view(np.int16)).view(torch.bfloat16)
+    one = torch.ones(1, device="cuda")
+    asp.shape_logits(x, draft_tokens=gpu(i32([[7, V - 1]])), repetition=2 * one, presence=one)
+    got = x.view(torch.int16).cpu().numpy().view(np.uint16)
+    changed = got != bits
+    assert not changed[0, 0].any()
+    assert changed[0, 1].nonzero()[0].tolist() == [7] and changed[0, 2].nonzero()[0].tolist() == [7, V - 1]
+    assert torch.isnan(x).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_shape_special_values(dtype):
     """Infinities and not-a-numbers under penalties and masks; biases of
