@@ -59,8 +59,8 @@ typedef struct asymspec_shape {
   void* out;                     /* the same for out_row_stride, out_request_stride.  Either
                                     `logits` itself with the same strides (in place: only
                                     16-byte pieces that change are read or written), or
-                                    memory that does not overlap it (all rows are written).
-                                    Rows of one tensor must not overlap each other          */
+                                    memory that begins behind its end or ends ahead of it
+                                    (all rows are written).  Rows of `out` lie apart         */
   int64_t request_stride, row_stride;
   int64_t out_request_stride, out_row_stride;
   const int32_t* history;        /* [B][max_history], or NULL: no history                    */
@@ -80,7 +80,7 @@ typedef struct asymspec_shape {
                                     token x is allowed; or NULL                               */
   const int32_t* mask_index;     /* [B][R]: the row of `mask`; out of range: no mask          */
   int32_t dtype;                 /* ASYMSPEC_BF16 or ASYMSPEC_FP32                            */
-  int32_t B, R, V;               /* B >= 1, R in [1, 64], V >= 1                              */
+  int32_t B, R, V;               /* B >= 1, R in [1, 64], V in [1, 2^30)                      */
   int32_t max_history;           /* row length of `history`; at most 1048575                  */
   int32_t D;                     /* 0, or in [R - 1, 64]                                       */
   int32_t n_ids;                 /* length of id_map                                          */

@@ -14,11 +14,13 @@
 // again to find the token.  A row is split because the exponentials bound it: one
 // compute unit alone would take about 20 us over 151936 tokens.
 //
-// draw_part runs 19 vector operations a token and about 100 a chunk, 25 a token in
-// all, at 33e12 lane operations a second as this chip issues fp64 ones: 99 us for
-// 512 rows of 256000 bf16 tokens (262 MB, 40 us at a read's rate), 15 us for 128 of
-// 151936.  Chunks of 2048 tokens take 4% less there, but 0.7 us more on one row
-// and in draw_pick; waves that stay and fetch their next chunk ahead take 4% more.
+// draw_part runs 20 vector operations a token and about 100 a chunk, 26 a token in
+// all, at 33e12 lane operations a second as this chip issues fp64 ones: 103 us for
+// 512 rows of 256000 bf16 tokens (262 MB, 51 us at a copy's rate; 95 us with the rows
+// in cache), 15 us for 128 of 151936; draw_pick 4 to 5 us.  Greedy rows take a read's
+// time.  Chunks of 2048 tokens take 4% less on the large batch, but 0.7 us more on one
+// row and in draw_pick; two chunks a wave, or waves that stay and fetch their next
+// chunk ahead, take 4 to 6% more (a SIMD then holds seven waves in place of eight).
 
 #ifndef ASYMSPEC_STEP_DRAW_H_
 #define ASYMSPEC_STEP_DRAW_H_
@@ -177,18 +179,33 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
   int32_t* token = A.token + row * A.token_stride;
   float* prob = A.prob ? A.prob + row * A.prob_stride : nullptr;
 
-  // The chunk that the draw falls into: each lane has a run of chunks.
+  // The chunk that the draw falls into: each lane has a run of chunks, kept in
+  // registers where it is short (rows of up to 2^18 tokens), else read each time.
+  constexpr int kKeep = 4;
   const int per = (A.S + 63) / 64;
   const int lo = min(A.S, lane * per), hi = min(A.S, lo + per);
+  DrawPart kept[kKeep];
+#pragma unroll
+  for (int j = 0; j < kKeep; ++j) kept[j] = per <= kKeep && lo + j < hi ? P[lo + j] : DrawPart{0.0, -inf, 0x7FFFFFFF};
+  auto each = [&](auto&& f) {       // f(chunk, its part), in order
+    if (per <= kKeep) {
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j) f(lo + j, kept[j]);
+    } else {
+      for (int s = lo; s < hi; ++s) {
+        DrawPart q = P[s];
+        f(s, q);
+      }
+    }
+  };
   float mine_m = -inf;
   int arg = 0x7FFFFFFF;
-  for (int s = lo; s < hi; ++s) {
-    const float x = P[s].m;
-    if (x > mine_m) {
-      mine_m = x;
-      arg = P[s].arg;
+  each([&](int, const DrawPart& q) {
+    if (q.m > mine_m) {
+      mine_m = q.m;
+      arg = q.arg;
     }
-  }
+  });
   const float m = asym::wave_max(mine_m);
   if (!(tau > 0.0f) || m == -inf) {
     arg = asym::wave_min_i(mine_m == m ? arg : 0x7FFFFFFF);
@@ -199,12 +216,13 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
     return;
   }
   const DrawScale k(tau, m);
-  auto chunk = [&](int s) {
-    const DrawPart q = P[s];
-    return q.sum * k.weight((double)(k.inf ? k.flat(q.m) : q.m));
-  };
+  auto weight_of = [&](const DrawPart& q) { return q.sum * k.weight((double)(k.inf ? k.flat(q.m) : q.m)); };
   double mine = 0.0, upto, ahead;
-  for (int s = lo; s < hi; ++s) mine += chunk(s);
+  each([&](int, DrawPart& q) {
+    const double w = weight_of(q);
+    q.sum = w;              // (of a kept part: its weight from here on)
+    mine += w;
+  });
   asym::wave_scan_d(mine, upto, ahead);
   const double total = __shfl(upto, 63, 64);
   const double target = (double)u * total;
@@ -215,18 +233,18 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
   const int from = none ? 63 - __clzll((long long)(some | 1ull)) : __ffsll(past) - 1;
   int at = lo;
   double before = ahead;
-  if (per > 1) {
+  {
     double c = ahead;
     bool found = false;
-    for (int s = lo; s < hi; ++s) {
-      const double w = chunk(s);
+    each([&](int s, const DrawPart& q) {
+      const double w = per <= kKeep ? q.sum : weight_of(q);
       if (w > 0.0 && !found) {
         at = s;
         before = c;
         found = !none && c + w > target;
       }
       c += w;
-    }
+    });
   }
   at = __shfl(at, from, 64);
   before = __shfl(before, from, 64);

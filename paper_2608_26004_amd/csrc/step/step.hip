@@ -4,9 +4,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <cstring>
-#include <mutex>
 
 #include "asymspec_step.h"
 #include "commit.h"
@@ -20,48 +20,63 @@ static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // Compute units of the current device, or 0 when it is no gfx950.
 static int device_cus() {
-  static std::mutex mu;
-  static int cus[64];       // 0: not looked at; -1: not a gfx950
+  static std::atomic<int> cus[64];       // 0: not looked at; -1: not a gfx950
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
     (void)hipGetLastError();
     return 0;
   }
-  std::lock_guard<std::mutex> lk(mu);
-  if (cus[dev] == 0) {
+  int n = cus[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
     hipDeviceProp_t pr;
     if (hipGetDeviceProperties(&pr, dev) != hipSuccess) {
       (void)hipGetLastError();
       return 0;
     }
-    cus[dev] = std::strncmp(pr.gcnArchName, "gfx950", 6) == 0 ? pr.multiProcessorCount : -1;
+    n = std::strncmp(pr.gcnArchName, "gfx950", 6) == 0 ? pr.multiProcessorCount : -1;
+    cus[dev].store(n, std::memory_order_relaxed);
   }
-  return std::max(cus[dev], 0);
+  return std::max(n, 0);
 }
 
-static int launched() {
-  if (hipGetLastError() == hipSuccess) return ASYMSPEC_OK;
+// Enqueues a kernel of one argument.
+template <class Args>
+static int launch(void (*kernel)(Args), unsigned grid, int threads, size_t lds, void* stream, Args& args) {
+  void* p[] = {&args};
+  if (hipLaunchKernel((const void*)kernel, dim3(grid), dim3(threads), p, lds, (hipStream_t)stream) == hipSuccess)
+    return ASYMSPEC_OK;
+  (void)hipGetLastError();
   return ASYMSPEC_E_DEVICE;
 }
 
-// Whether the rows of a [B][R][V] tensor lie apart, in one order or the other,
-// and its last element within 2^62 of the first.
+// Elements from the first to behind the last of a [B][R][V] tensor, or -1 when a
+// stride is negative or the tensor larger than any memory.
+static int64_t extent(int64_t B, int64_t R, int64_t V, int64_t sb, int64_t sr) {
+  if (sb < 0 || sr < 0) return -1;
+  const __int128 n = (__int128)(B - 1) * sb + (__int128)(R - 1) * sr + V;
+  return n > ((__int128)1 << 56) ? -1 : (int64_t)n;
+}
+
+// Whether its rows lie apart, in one order or the other.
 static bool rows_apart(int64_t B, int64_t R, int64_t V, int64_t sb, int64_t sr) {
-  if (sb < 0 || sr < 0) return false;
-  const __int128 span = (__int128)(B - 1) * sb + (__int128)(R - 1) * sr + V;
-  if (span > ((__int128)1 << 60)) return false;
   const bool request_major = (R == 1 || sr >= V) && (B == 1 || sb >= (R - 1) * sr + V);
   const bool row_major = (B == 1 || sb >= V) && (R == 1 || sr >= (B - 1) * sb + V);
   return request_major || row_major;
 }
 
 template <int DT>
-static void shape_launch(const ShapeArgs& A, unsigned grid, size_t lds, hipStream_t st) {
+static int shape_launch(ShapeArgs& A, unsigned grid, size_t lds, void* st) {
   const bool in_place = A.s.logits == A.s.out, masked = A.s.mask != nullptr;
-  if (in_place && masked) shape_kernel<DT, true, true><<<grid, kShapeThreads, lds, st>>>(A);
-  else if (in_place) shape_kernel<DT, true, false><<<grid, kShapeThreads, lds, st>>>(A);
-  else if (masked) shape_kernel<DT, false, true><<<grid, kShapeThreads, lds, st>>>(A);
-  else shape_kernel<DT, false, false><<<grid, kShapeThreads, lds, st>>>(A);
+  auto* kernel = in_place ? (masked ? shape_kernel<DT, true, true> : shape_kernel<DT, true, false>)
+                          : (masked ? shape_kernel<DT, false, true> : shape_kernel<DT, false, false>);
+  return launch(kernel, grid, kShapeThreads, lds, st, A);
+}
+
+template <int DT>
+static int draw_launch(DrawArgs& A, void* st) {
+  const unsigned grid = (unsigned)(((long long)A.N * A.S + kDrawThreads / 64 - 1) / (kDrawThreads / 64));
+  const int rc = launch(draw_part_kernel<DT>, grid, kDrawThreads, 0, st, A);
+  return rc != ASYMSPEC_OK ? rc : launch(draw_pick_kernel<DT>, (unsigned)A.N, 64, 0, st, A);
 }
 
 // Workspace of a draw; chunks of a row in *S.  0 for invalid arguments.
@@ -84,16 +99,21 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   A.s = *shape;
   asymspec_shape& s = A.s;
   if (s.dtype != ASYMSPEC_BF16 && s.dtype != ASYMSPEC_FP32) return ASYMSPEC_E_ARG;
-  if (s.B < 1 || s.R < 1 || s.R > ASYMSPEC_SHAPE_MAX_ROWS || s.V < 1) return ASYMSPEC_E_ARG;
+  if (s.B < 1 || s.R < 1 || s.R > ASYMSPEC_SHAPE_MAX_ROWS || s.V < 1 || s.V >= (1 << 30)) return ASYMSPEC_E_ARG;
   if (s.logits == nullptr || s.out == nullptr) return ASYMSPEC_E_ARG;
   // the row strides of one row, and the request strides of one request, do not matter
   if (s.R == 1) s.row_stride = s.out_row_stride = 0;
   if (s.B == 1) s.request_stride = s.out_request_stride = 0;
-  if (s.request_stride < 0 || s.row_stride < 0 || s.request_stride > (1ll << 40) || s.row_stride > (1ll << 40))
+  const size_t el = s.dtype == ASYMSPEC_BF16 ? 2 : 4;
+  const int64_t n_in = extent(s.B, s.R, s.V, s.request_stride, s.row_stride);
+  const int64_t n_out = extent(s.B, s.R, s.V, s.out_request_stride, s.out_row_stride);
+  if (n_in < 0 || n_out < 0 || !rows_apart(s.B, s.R, s.V, s.out_request_stride, s.out_row_stride)) return ASYMSPEC_E_ARG;
+  if (s.logits == s.out) {
+    if (s.request_stride != s.out_request_stride || s.row_stride != s.out_row_stride) return ASYMSPEC_E_ARG;
+  } else if ((uintptr_t)s.logits < (uintptr_t)s.out + (uintptr_t)n_out * el &&
+             (uintptr_t)s.out < (uintptr_t)s.logits + (uintptr_t)n_in * el) {
     return ASYMSPEC_E_ARG;
-  if (!rows_apart(s.B, s.R, s.V, s.out_request_stride, s.out_row_stride)) return ASYMSPEC_E_ARG;
-  if (s.logits == s.out && (s.request_stride != s.out_request_stride || s.row_stride != s.out_row_stride))
-    return ASYMSPEC_E_ARG;
+  }
   if (s.history != nullptr) {
     if (s.lengths == nullptr || s.max_history < 1 || s.max_history > ASYMSPEC_SHAPE_MAX_HISTORY) return ASYMSPEC_E_ARG;
   } else {
@@ -110,7 +130,6 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   if (s.n_bias < 0 || s.n_bias > ASYMSPEC_SHAPE_MAX_BIAS) return ASYMSPEC_E_ARG;
   if ((s.mask == nullptr) != (s.mask_index == nullptr)) return ASYMSPEC_E_ARG;
   if (s.mask != nullptr && s.n_masks < 0) return ASYMSPEC_E_ARG;
-  const size_t el = s.dtype == ASYMSPEC_BF16 ? 2 : 4;
   if (!aligned(s.logits, el) || !aligned(s.out, el)) return ASYMSPEC_E_ALIGN;
   for (const void* p : {(const void*)s.history, (const void*)s.lengths, (const void*)s.prompt_lengths,
                         (const void*)s.draft_tokens, (const void*)s.id_map, (const void*)s.repetition,
@@ -133,9 +152,8 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   const long long grid = (long long)s.B * A.parts;
   if (grid > 0x7FFFFFFFll) return ASYMSPEC_E_ARG;
   const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T) : ShapeLds<4>::bytes(T);
-  if (s.dtype == ASYMSPEC_BF16) shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, (hipStream_t)stream);
-  else shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, (hipStream_t)stream);
-  return launched();
+  return s.dtype == ASYMSPEC_BF16 ? shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, stream)
+                                  : shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, stream);
 }
 
 size_t asymspec_draw_workspace_size(int N, int V, int dtype) {
@@ -176,16 +194,7 @@ int asymspec_draw_tokens(const void* logits, int dtype, int N, int V, int64_t ro
   A.part = (DrawPart*)workspace;
   A.N = N;
   A.V = V;
-  hipStream_t st = (hipStream_t)stream;
-  const unsigned grid = (unsigned)(((long long)N * A.S + kDrawThreads / 64 - 1) / (kDrawThreads / 64));
-  if (dtype == ASYMSPEC_BF16) {
-    draw_part_kernel<ASYMSPEC_BF16><<<grid, kDrawThreads, 0, st>>>(A);
-    draw_pick_kernel<ASYMSPEC_BF16><<<N, 64, 0, st>>>(A);
-  } else {
-    draw_part_kernel<ASYMSPEC_FP32><<<grid, kDrawThreads, 0, st>>>(A);
-    draw_pick_kernel<ASYMSPEC_FP32><<<N, 64, 0, st>>>(A);
-  }
-  return launched();
+  return dtype == ASYMSPEC_BF16 ? draw_launch<ASYMSPEC_BF16>(A, stream) : draw_launch<ASYMSPEC_FP32>(A, stream);
 }
 
 int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token, const int32_t* draft_tokens,
@@ -212,8 +221,7 @@ int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token,
   A.max_lengths = max_lengths; A.lengths_out = lengths_out; A.finished_out = finished_out;
   A.tokens_out = tokens_out; A.counts_out = counts_out;
   A.max_history = max_history; A.n_stop = n_stop; A.B = B; A.K = K;
-  commit_kernel<<<(unsigned)((B + kCommitPer - 1) / kCommitPer), kCommitThreads, 0, (hipStream_t)stream>>>(A);
-  return launched();
+  return launch(commit_kernel, (unsigned)((B + kCommitPer - 1) / kCommitPer), kCommitThreads, 0, stream, A);
 }
 
 int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const int32_t* release,
@@ -250,8 +258,7 @@ int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const
   // not know: a request that ends gives all it has, so one table in 32.
   const long long entries = places + places / 8 + (long long)B * max_blocks / 32;
   const long long grid = std::min<long long>(entries / kSlotsThreads + 1, 2ll * cus);
-  slots_kernel<<<(unsigned)grid, kSlotsThreads, (size_t)(4 * (B + 1)) * 4, (hipStream_t)stream>>>(A);
-  return launched();
+  return launch(slots_kernel, (unsigned)grid, kSlotsThreads, (size_t)(4 * (B + 1)) * 4, stream, A);
 }
 
 }  // extern "C"

@@ -68,6 +68,9 @@ def shape_call(**over):
 @pytest.mark.parametrize("over,code", [
     (dict(logits=None), asp.E_ARG), (dict(out=None), asp.E_ARG), (dict(dtype=2), asp.E_ARG),
     (dict(B=0), asp.E_ARG), (dict(R=0), asp.E_ARG), (dict(R=65), asp.E_ARG), (dict(V=0), asp.E_ARG),
+    (dict(V=1 << 30, R=1, B=1, D=0), asp.E_ARG), (dict(request_stride=1 << 55, out_request_stride=1 << 55), asp.E_ARG),
+    # out of place, but not apart: a part of it, and the next rows
+    (dict(out=FAKE + 400), asp.E_ARG), (dict(out=FAKE + 4 * 1199), asp.E_ARG), (dict(logits=FAKE + 4 * 1199), asp.E_ARG),
     (dict(lengths=None), asp.E_ARG), (dict(max_history=0), asp.E_ARG), (dict(max_history=1 << 20), asp.E_ARG),
     (dict(D=-1), asp.E_ARG), (dict(D=1), asp.E_ARG), (dict(D=65), asp.E_ARG), (dict(draft_stride=-1), asp.E_ARG),
     (dict(bias_values=None), asp.E_ARG), (dict(n_bias=1024), asp.E_ARG), (dict(n_bias=-1), asp.E_ARG),
@@ -95,6 +98,8 @@ def test_shape_refusals(over, code):
     dict(R=1, D=0, row_stride=-9, out_row_stride=1),
     # rows outside requests: [R][B][V]
     dict(request_stride=100, row_stride=400, out_request_stride=100, out_row_stride=400),
+    # right behind, and right ahead
+    dict(out=FAKE + 4 * 1200), dict(logits=FAKE + 4 * 1200),
     # a repeated input row is fine out of place
     dict(out=FAKE * 2, request_stride=0, row_stride=0)])
 def test_shape_accepts(over):
