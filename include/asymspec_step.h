@@ -80,7 +80,8 @@ typedef struct asymspec_shape {
                                     token x is allowed; or NULL                               */
   const int32_t* mask_index;     /* [B][R]: the row of `mask`; out of range: no mask          */
   int32_t dtype;                 /* ASYMSPEC_BF16 or ASYMSPEC_FP32                            */
-  int32_t B, R, V;               /* B >= 1, R in [1, 64], V in [1, 2^30)                      */
+  int32_t B, R, V;               /* B >= 1, R in [1, 64], V in [1, 2^30); B * ceil(V / 8192)
+                                    below 2^23 - 1                                            */
   int32_t max_history;           /* row length of `history`; at most 1048575                  */
   int32_t D;                     /* 0, or in [R - 1, 64]                                       */
   int32_t n_ids;                 /* length of id_map                                          */
@@ -114,8 +115,12 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream);
  *   prob         [N] out, prob_stride elements apart; or NULL
  *   workspace    >= asymspec_draw_workspace_size bytes, 16-byte aligned;
  *                needs no initialisation; calls that may run at the same time
- *                need distinct ones
- * N >= 1, 1 <= V < 2^30.
+ *                (replays of a captured one among them) need distinct ones.  A
+ *                draw leaves anything there, so memory that asymspec_fuse_verify
+ *                works in is cleared in between (asymspec_workspace_clear)
+ * The outputs and the workspace overlap no other array.  N >= 1, 1 <= V < 2^30,
+ * N * ceil(V / 1024) below 2^26 - 4 (a size of 0 bytes says that a shape is not
+ * valid).
  */
 size_t asymspec_draw_workspace_size(int N, int V, int dtype);
 int asymspec_draw_tokens(const void* logits, int dtype, int N, int V, int64_t row_stride,
@@ -143,8 +148,9 @@ int asymspec_draw_tokens(const void* logits, int dtype, int N, int V, int64_t ro
  *                  token, or (with accept_len in [0, K]) is at its limit; else 0
  *   tokens_out     [B][K + 1] out: the committed tokens, then -1
  *   counts_out     [B] out: how many
- * The outputs overlap no input, except that lengths_out may be lengths and
- * finished_out finished.  B >= 1, 0 <= K <= 63.
+ * The outputs overlap one another and the inputs nowhere, except that
+ * lengths_out may be lengths and finished_out finished.  1 <= B < 2^26 - 4,
+ * 0 <= K <= 63.
  */
 int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token,
                            const int32_t* draft_tokens, int64_t draft_stride,

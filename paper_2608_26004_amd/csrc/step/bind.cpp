@@ -317,14 +317,9 @@ struct DrawShape {
   }
 };
 
-// logits -> bytes of workspace
-PyObject* draw_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 1, [&] { return PyLong_FromSize_t(DrawShape(given("logits", a[0])).bytes()); });
-}
-
-// logits, temperature, uniforms, out, workspace tensor or None, stream
+// logits, temperature, uniforms, out, stream
 PyObject* draw_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 6, [&]() -> PyObject* {
+  return guarded(n, 5, [&]() -> PyObject* {
     const Tensor& x = given("logits", a[0]);
     const DrawShape d(x);
     const at::Device dev = x.device();
@@ -336,18 +331,20 @@ PyObject* draw_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     out.is(at::kInt, N);
     out.is(at::kFloat, N);
     const OnDevice on(dev);
-    size_t bytes = d.bytes();
-    const Tensor* given_ws = tensor("workspace", a[4]);
-    void* ws = out.make(dev, given_ws != nullptr ? 0 : bytes);
-    if (given_ws != nullptr) {
-      if (given_ws->device() != dev || !given_ws->is_contiguous()) refuse("workspace must be memory of the logits' device");
-      ws = given_ws->data_ptr();
-      bytes = given_ws->nbytes();
+    const size_t bytes = d.bytes();
+    // A small workspace shares the outputs' allocation, which lives as long as they
+    // do; a large one, which a draw of some time has, is given back at once.
+    const bool small = bytes <= (16u << 10);
+    void* ws = out.make(dev, small ? bytes : 0);
+    Tensor own_ws;
+    if (!small) {
+      own_ws = at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(dev));
+      ws = own_ws.data_ptr();
     }
     int* token = out.ptr<int>("token", 0, dev, false);
     float* prob = out.ptr<float>("q", 1, dev, false);
     check(asymspec_draw_tokens(x.data_ptr(), d.type, (int)N, (int)d.V, x.stride(0), tp, up, u.stride(0), token,
-                               out.at[0]->stride(0), prob, out.at[1]->stride(0), ws, bytes, stream_of(a[5])));
+                               out.at[0]->stride(0), prob, out.at[1]->stride(0), ws, bytes, stream_of(a[4])));
     return out.result();
   });
 }
@@ -441,7 +438,6 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 PyMethodDef methods[] = {
     {"shape_logits", (PyCFunction)(void (*)(void))shape_logits, METH_FASTCALL, nullptr},
-    {"draw_workspace", (PyCFunction)(void (*)(void))draw_workspace, METH_FASTCALL, nullptr},
     {"draw_tokens", (PyCFunction)(void (*)(void))draw_tokens, METH_FASTCALL, nullptr},
     {"commit_tokens", (PyCFunction)(void (*)(void))commit_tokens, METH_FASTCALL, nullptr},
     {"plan_slots", (PyCFunction)(void (*)(void))plan_slots, METH_FASTCALL, nullptr},

@@ -39,6 +39,9 @@ static int device_cus() {
   return std::max(n, 0);
 }
 
+// A launch has fewer than 2^32 threads.
+static bool fits(long long grid, int threads) { return grid <= 0xFFFFFFFFll / threads; }
+
 // Enqueues a kernel of one argument.
 template <class Args>
 static int launch(void (*kernel)(Args), unsigned grid, int threads, size_t lds, void* stream, Args& args) {
@@ -83,7 +86,7 @@ static int draw_launch(DrawArgs& A, void* st) {
 static size_t draw_bytes(int N, int V, int dtype, int* S) {
   if (N < 1 || V < 1 || V >= (1 << 30) || (dtype != ASYMSPEC_BF16 && dtype != ASYMSPEC_FP32)) return 0;
   *S = (V + kDrawChunk - 1) / kDrawChunk;
-  if ((long long)N * *S > 0x7FFFFFFFll) return 0;
+  if (!fits((long long)N * *S + kDrawThreads / 64, 64)) return 0;
   return (size_t)N * *S * sizeof(DrawPart);
 }
 
@@ -130,6 +133,8 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   if (s.n_bias < 0 || s.n_bias > ASYMSPEC_SHAPE_MAX_BIAS) return ASYMSPEC_E_ARG;
   if ((s.mask == nullptr) != (s.mask_index == nullptr)) return ASYMSPEC_E_ARG;
   if (s.mask != nullptr && s.n_masks < 0) return ASYMSPEC_E_ARG;
+  // (of the longest parts: shorter ones are taken for few workgroups only)
+  if (!fits((long long)s.B * ((s.V + kShapeMaxTokens - 1) / kShapeMaxTokens), kShapeThreads)) return ASYMSPEC_E_ARG;
   if (!aligned(s.logits, el) || !aligned(s.out, el)) return ASYMSPEC_E_ALIGN;
   for (const void* p : {(const void*)s.history, (const void*)s.lengths, (const void*)s.prompt_lengths,
                         (const void*)s.draft_tokens, (const void*)s.id_map, (const void*)s.repetition,
@@ -150,7 +155,6 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   A.lgT = __builtin_ctz((unsigned)T);
   A.parts = (s.V + T - 1) / T;
   const long long grid = (long long)s.B * A.parts;
-  if (grid > 0x7FFFFFFFll) return ASYMSPEC_E_ARG;
   const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T) : ShapeLds<4>::bytes(T);
   return s.dtype == ASYMSPEC_BF16 ? shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, stream)
                                   : shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, stream);
@@ -202,7 +206,8 @@ int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token,
                            const int32_t* finished, const int32_t* stop_tokens, int n_stop,
                            const int32_t* max_lengths, int B, int K, int32_t* lengths_out, int32_t* finished_out,
                            int32_t* tokens_out, int32_t* counts_out, void* stream) {
-  if (B < 1 || K < 0 || K > 63 || max_history < 1 || n_stop < 0) return ASYMSPEC_E_ARG;
+  if (B < 1 || !fits((long long)B + kCommitPer, 64) || K < 0 || K > 63 || max_history < 1 || n_stop < 0)
+    return ASYMSPEC_E_ARG;
   if (accept_len == nullptr || next_token == nullptr || history == nullptr || lengths == nullptr ||
       lengths_out == nullptr || finished_out == nullptr || tokens_out == nullptr || counts_out == nullptr)
     return ASYMSPEC_E_ARG;

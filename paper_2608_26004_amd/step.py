@@ -51,7 +51,7 @@ def shape_logits(logits, history=None, lengths=None, prompt_lengths=None, draft_
 
     logits: [B, R, V] bfloat16 or float32, the last dimension contiguous (rows
     may be strided views, such as one position of a [B, K+1, V] buffer);
-    history: [B, L] tokens of each request, lengths: [B] how many of them,
+    history: [B, L] tokens of each request (L below 2^20), lengths: [B] how many of them,
     prompt_lengths: [B] how many of those are its prompt (seen, but not counted);
     draft_tokens: [B, D]: row r follows the history and the first D - (R - 1) + r
     drafts (with R = K + 1 and D = K: row r the first r, as fuse_verify's rows;
@@ -63,7 +63,8 @@ def shape_logits(logits, history=None, lengths=None, prompt_lengths=None, draft_
     allowed, mask_index: [B, R] its row for each logit row (out of range: none);
     id_map: [n_ids]: history and drafts are ids of another vocabulary, whose id x
     is id_map[x] here (out of range: none);
-    out: None shapes `logits` in place, else a tensor of the same shape and dtype.
+    out: None shapes `logits` in place, else a tensor of the same shape and dtype
+    in other memory.
     With c occurrences among the output tokens and drafts ahead of the row, a
     logit v becomes, in fp32: v / repetition (v > 0) or v * repetition if the
     token occurs there or in the prompt; minus frequency * c and minus presence
@@ -73,7 +74,7 @@ def shape_logits(logits, history=None, lengths=None, prompt_lengths=None, draft_
                                            out, _stream(logits))
 
 
-def draw_tokens(logits, temperature, uniforms, out=None, workspace=None):
+def draw_tokens(logits, temperature, uniforms, out=None):
     """The drafter's own choice from each row: (token [N] int32, q(token) [N]
     float32).
 
@@ -82,13 +83,11 @@ def draw_tokens(logits, temperature, uniforms, out=None, workspace=None):
     (<= 0: the lowest index of the largest logit, q = 1); uniforms: [N] float32 in
     [0, 1), for an inverse-CDF draw from softmax(logits / temperature), summed in
     fp64; out: (token, q) tensors to write, views such as draft_tokens[:, i]
-    among them; workspace: a Workspace (by default memory of the call's own).
-    Logits of -inf or not a number have no weight; a row without any gives
-    token 0 with q = 0."""
-    step = _step or _bind()
-    if workspace is not None:
-        workspace = workspace.get(step.draw_workspace(logits), logits.device)
-    return step.draw_tokens(logits, temperature, uniforms, out, workspace, _stream(logits))
+    among them.  Logits of -inf or not a number have no weight; a row without any
+    gives token 0 with q = 0.  The workspace is memory of the call's own, from
+    torch's allocator: a Workspace holds what fuse_verify knows again, and a
+    captured call must not work in memory that a later one replaces."""
+    return (_step or _bind()).draw_tokens(logits, temperature, uniforms, out, _stream(logits))
 
 
 def commit_tokens(accept_len, next_token, draft_tokens, history, lengths, finished=None, stop_tokens=None,
@@ -111,7 +110,7 @@ def plan_slots(lengths, new_tokens, block_table, n_blocks, free_ring, free_state
                width=None, total=None, release=None, out=None):
     """Cache blocks and slots for the requests' next tokens.
 
-    Request b has lengths[b] tokens in its cache and gets new_tokens[b] more
+    Request b of at most 4096 has lengths[b] tokens in its cache and gets new_tokens[b] more
     ([B], or None: `width` each); blocks it lacks are taken from the front of
     free_ring, blocks beyond its need (all with release[b]) go back to the end.
     block_table: [B, max_blocks] and free_ring: [pool] are changed in place;

@@ -76,6 +76,9 @@ def shape_call(**over):
     (dict(bias_values=None), asp.E_ARG), (dict(n_bias=1024), asp.E_ARG), (dict(n_bias=-1), asp.E_ARG),
     (dict(mask_index=None), asp.E_ARG), (dict(mask=None), asp.E_ARG), (dict(n_masks=-1), asp.E_ARG),
     (dict(id_map=FAKE, n_ids=-1), asp.E_ARG),
+    # more threads than a launch has
+    (dict(B=1 << 23, R=1, D=0), asp.E_ARG), (dict(B=1 << 10, R=1, D=0, V=1 << 26, request_stride=1 << 26,
+                                                  out_request_stride=1 << 26), asp.E_ARG),
     # in place with other strides; rows of one tensor that overlap
     (dict(out_row_stride=101, out_request_stride=303), asp.E_ARG),
     (dict(row_stride=99, out_row_stride=99), asp.E_ARG),
@@ -119,7 +122,8 @@ def draw_call(**over):
 @pytest.mark.parametrize("over,code", [
     (dict(logits=None), asp.E_ARG), (dict(tau=None), asp.E_ARG), (dict(token=None), asp.E_ARG),
     (dict(ws=None), asp.E_ARG), (dict(dtype=9), asp.E_ARG), (dict(N=0), asp.E_ARG), (dict(V=0), asp.E_ARG),
-    (dict(V=1 << 30), asp.E_ARG), (dict(N=1 << 30), asp.E_ARG), (dict(stride=-1), asp.E_ARG),
+    (dict(V=1 << 30), asp.E_ARG), (dict(N=1 << 30), asp.E_ARG),
+    (dict(N=1 << 26, V=1, wsb=1 << 40), asp.E_ARG), (dict(stride=-1), asp.E_ARG),
     (dict(ts=0), asp.E_ARG), (dict(ps=0), asp.E_ARG), (dict(us=-1), asp.E_ARG),
     (dict(logits=FAKE + 1), asp.E_ALIGN), (dict(dtype=asp.FP32, logits=ODD), asp.E_ALIGN),
     (dict(prob=ODD), asp.E_ALIGN), (dict(ws=FAKE + 8), asp.E_ALIGN), (dict(wsb=32), asp.E_WORKSPACE),
@@ -131,7 +135,8 @@ def test_draw_refusals(over, code):
 def test_draw_workspace_size():
     size = library().asymspec_draw_workspace_size
     assert size(1, 1, asp.FP32) > 0 and size(4, 100000, asp.BF16) == 4 * size(1, 100000, asp.BF16)
-    for bad in ((0, 5, 0), (1, 0, 0), (1, 1 << 30, 0), (1, 5, 2), (-1, 5, 0)):
+    assert size((1 << 26) - 5, 1024, 0) == ((1 << 26) - 5) * size(1, 1, 0)
+    for bad in ((1 << 26, 5, 0), ((1 << 25), 1025, 0), (0, 5, 0), (1, 0, 0), (1, 1 << 30, 0), (1, 5, 2), (-1, 5, 0)):
         assert size(*bad) == 0
 
 
@@ -146,7 +151,7 @@ def commit_call(**over):
     (dict(acc=None), asp.E_ARG), (dict(nxt=None), asp.E_ARG), (dict(d=None), asp.E_ARG), (dict(hist=None), asp.E_ARG),
     (dict(lens=None), asp.E_ARG), (dict(lo=None), asp.E_ARG), (dict(fo=None), asp.E_ARG), (dict(to=None), asp.E_ARG),
     (dict(co=None), asp.E_ARG), (dict(stops=None), asp.E_ARG), (dict(n_stop=-1), asp.E_ARG), (dict(B=0), asp.E_ARG),
-    (dict(K=-1), asp.E_ARG), (dict(K=64), asp.E_ARG), (dict(L=0), asp.E_ARG), (dict(ds=-1), asp.E_ARG),
+    (dict(B=1 << 26), asp.E_ARG), (dict(K=-1), asp.E_ARG), (dict(K=64), asp.E_ARG), (dict(L=0), asp.E_ARG), (dict(ds=-1), asp.E_ARG),
     (dict(hist=ODD), asp.E_ALIGN), (dict(co=ODD), asp.E_ALIGN),
 ])
 def test_commit_refusals(over, code):

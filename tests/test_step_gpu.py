@@ -278,7 +278,7 @@ def test_draw_every_kind_of_not_a_number():
 
 def test_draw_strided_views_and_out():
     """One position of the rows' buffer in, columns of [B][K] buffers out; the
-    other columns stay; the same bits with a workspace and without, twice."""
+    other columns stay; the same bits as from rows on their own."""
     rng = np.random.default_rng(3)
     B, K, V = 9, 4, 5001
     buf, _ = stored(rng, (B, K + 1, V), "bf16")
@@ -286,12 +286,19 @@ def test_draw_strided_views_and_out():
     uni = torch.from_numpy(rng.random((B, K), dtype=np.float32)).cuda()
     d = torch.full((B, K), -7, dtype=torch.int32, device="cuda")
     q = torch.full((B, K), -7.0, device="cuda")
-    ws = asp.Workspace(torch.device("cuda", 0))
     for i in range(K):
         want = asp.draw_tokens(buf[:, i].contiguous(), gpu(tau), uni[:, i].contiguous())
-        asp.draw_tokens(buf[:, i], gpu(tau), uni[:, i], out=(d[:, i], q[:, i]), workspace=ws)
+        asp.draw_tokens(buf[:, i], gpu(tau), uni[:, i], out=(d[:, i], q[:, i]))
         assert torch.equal(d[:, i], want[0]) and torch.equal(q[:, i], want[1])
         assert (d[:, i + 1:] == -7).all() and (q[:, i + 1:] == -7).all()
+
+
+def test_draw_outputs_keep_no_large_memory():
+    """Tokens that a program keeps do not keep the call's workspace."""
+    x = torch.zeros(64, 40000, dtype=torch.bfloat16, device="cuda")
+    one = torch.ones(64, device="cuda")
+    tok, q = asp.draw_tokens(x, one, one)
+    assert max(tok.untyped_storage().nbytes(), q.untyped_storage().nbytes()) <= 1 << 15
 
 
 def test_draw_follows_the_distribution():
