@@ -77,8 +77,18 @@ static int shape_launch(ShapeArgs& A, unsigned grid, size_t lds, void* st) {
 
 template <int DT>
 static int draw_launch(DrawArgs& A, void* st) {
-  const unsigned grid = (unsigned)(((long long)A.N * A.S + kDrawThreads / 64 - 1) / (kDrawThreads / 64));
-  const int rc = launch(draw_part_kernel<DT>, grid, kDrawThreads, 0, st, A);
+  // With a table as many workgroups as are resident at once (two a unit), each with
+  // chunks of one row.
+  const int wide = std::max(1, 2 * device_cus() / A.N);
+  A.C = std::min((A.S + wide - 1) / wide, kTableMost);
+  A.P = (A.S + A.C - 1) / A.C;
+  int rc;
+  if (DT == ASYMSPEC_BF16 && A.C >= kTableChunks) {
+    rc = launch(draw_table_kernel, (unsigned)(A.N * A.P), kTableThreads, 0, st, A);
+  } else {
+    const unsigned grid = (unsigned)(((long long)A.N * A.S + kDrawThreads / 64 - 1) / (kDrawThreads / 64));
+    rc = launch(draw_part_kernel<DT>, grid, kDrawThreads, 0, st, A);
+  }
   return rc != ASYMSPEC_OK ? rc : launch(draw_pick_kernel<DT>, (unsigned)A.N, 64, 0, st, A);
 }
 

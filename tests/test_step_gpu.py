@@ -265,6 +265,53 @@ def test_draw_special_rows():
     assert tok[12] == 7999 and tok[13] == V - 1 and tok[14] == 3 and tok[15] == 0
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("offset", [0.0, 1e4, -1e4, 1e30, -1e30])
+def test_draw_kinds_of_chunks(offset, dtype):
+    """1024 tokens each: all negative, mixed, with -inf, spread wide, with a
+    not-a-number, all positive, negative zeros, a part; at temperatures from those
+    that leave one token to those that leave all."""
+    rng = np.random.default_rng(7)
+    N, V = 24, 7 * 1024 + 300
+    l = rng.normal(0, 3, (N, V))
+    l[:, :1024] = -np.abs(l[:, :1024]) - 0.5
+    l[:, 2048 + 5:3072:7] = -np.inf
+    l[:, 3072:4096] *= 300.0
+    l[:, 4096 + 9] = np.nan
+    l[:, 5120:6144] = np.abs(l[:, 5120:6144]) + 0.5
+    l[:, 6144:7168] = -0.0
+    l[1::3, 3072:4096] = -900.0                 # the wide chunk without the largest one
+    x = gpu((l + offset).astype(np.float32)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    tau = np.tile(np.float32([0.0, 0.01, 0.4, 1.0, 20.0, 1e4, 1e32, math.inf]), 3)
+    check_draw(x, tau, rng.random(N, dtype=np.float32))
+
+
+@pytest.mark.parametrize("N,V", [(300, 40000), (1500, 17000), (70, 151936), (3, 5000000)])
+def test_draw_of_many_tokens(N, V):
+    """Large bf16 draws, and a few rows among them with chunks of every kind: each
+    row as alone (a row's result does not depend on how many there are), and the
+    first ones as the reference has them."""
+    rng = np.random.default_rng(N)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x = (torch.randn(N, V, generator=g, device="cuda") * 3).to(torch.bfloat16)
+    x[1, 1024 * 3 + 7] = 0.0
+    x[2, 5000 - 900:5000] = -math.inf
+    x[3 % N, ::3] = -math.inf
+    x[4 % N, 77], x[5 % N, 4900] = math.nan, 200.0
+    x[6 % N] *= 100.0
+    x[7 % N, 1024:2048] = -150.0
+    if N > 8:
+        x[7, 2048:4096], x[8] = -math.inf, -math.inf
+    tau = rng.choice(np.float32([0.0, 0.1, 0.5, 1.0, 2.0, math.inf]), N).astype(np.float32)
+    tau[:9] = np.float32([1.0, 0.8, 0.3, 1.0, 0.19, 2.0, 1.0, 0.6, 3e9])[:min(N, 9)]
+    u = rng.random(N, dtype=np.float32)
+    tok, q = asp.draw_tokens(x, gpu(tau), gpu(u))
+    for n in list(range(min(N, 9))) + [N - 1]:
+        check_draw(x[n:n + 1], tau[n:n + 1], u[n:n + 1])
+        t1, q1 = asp.draw_tokens(x[n:n + 1], gpu(tau[n:n + 1]), gpu(u[n:n + 1]))
+        assert tok[n] == t1[0] and abs(q[n] - q1[0]) <= 2.0 ** -23 * q1[0]
+
+
 def test_draw_every_kind_of_not_a_number():
     """Quiet and signalling ones of either sign, as bf16 bit patterns."""
     V = 5000
