@@ -21,8 +21,8 @@
 // a read's time.  Chunks of 2048 tokens take 4% less on the large batch, but 0.7 us more
 // on one row and in draw_pick; two chunks a wave, or waves that stay and fetch their next
 // chunk ahead, take 4 to 6% more (a SIMD then holds seven waves in place of eight).
-// draw_table takes 58 us there, which is a read's time; of 128 rows of 151936 tokens 13 us
-// against 14, of which 2 are the table's making.  draw_pick takes 4 to 5 us.
+// draw_table takes 55 to 60 us there, near a read's time; for 128 rows of 151936 tokens 13 us
+// against 16, 1 to 2 of them the table's making.  draw_pick takes 4 to 5 us.
 
 #ifndef ASYMSPEC_STEP_DRAW_H_
 #define ASYMSPEC_STEP_DRAW_H_
