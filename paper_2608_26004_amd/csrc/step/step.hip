@@ -143,8 +143,8 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   if (s.n_bias < 0 || s.n_bias > ASYMSPEC_SHAPE_MAX_BIAS) return ASYMSPEC_E_ARG;
   if ((s.mask == nullptr) != (s.mask_index == nullptr)) return ASYMSPEC_E_ARG;
   if (s.mask != nullptr && s.n_masks < 0) return ASYMSPEC_E_ARG;
-  // (of the longest parts: shorter ones are taken for few workgroups only)
-  if (!fits((long long)s.B * ((s.V + kShapeMaxTokens - 1) / kShapeMaxTokens), kShapeThreads)) return ASYMSPEC_E_ARG;
+  auto workgroups = [&](int T) { return (long long)s.B * ((s.V + T - 1) / T); };
+  if (!fits(workgroups(kShapeMaxTokens), kShapeThreads)) return ASYMSPEC_E_ARG;
   if (!aligned(s.logits, el) || !aligned(s.out, el)) return ASYMSPEC_E_ALIGN;
   for (const void* p : {(const void*)s.history, (const void*)s.lengths, (const void*)s.prompt_lengths,
                         (const void*)s.draft_tokens, (const void*)s.id_map, (const void*)s.repetition,
@@ -153,18 +153,22 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
     if (!aligned(p, 4)) return ASYMSPEC_E_ALIGN;
   const int cus = device_cus();
   if (cus == 0) return ASYMSPEC_E_DEVICE;
-  // The shortest parts that do not make too many workgroups, since each reads the
-  // request's lists again.  In place, as many as are resident at once (four a unit):
-  // 8 x 3 rows of 151936 bf16 tokens behind 4096: 9.2 us at 600 workgroups, 10.4 at
-  // 1192 and 10.0 at 304.  A copy wants about five times as many, so that some copy
-  // while others list: 96 x 6 rows of 50257 fp32 tokens 64 us at 4800 workgroups, 79 at
-  // 672; 64 x 5 rows of 151936 bf16 tokens behind 8192 61 us at 4800, 89 at 9536, 71 at 1216.
-  const long long most = (s.logits == s.out ? 4ll : 20ll) * cus;
+  // A workgroup's lists cost the same however few tokens it has, and some copy or mask
+  // while others list.  So parts grow until a workgroup has enough to do: 20 KB of rows to
+  // copy, 40 KB under masks, and what there is where only listed vectors change; but not
+  // to two workgroups a unit or fewer.  Copies: 96 x 6 rows of 50257 fp32 tokens 58 us
+  // with 24 KB, 63 with 48; 128 x 1 of 151936 bf16 24 with 16 KB, 36 with 8; 16 x 3 of 256000
+  // behind 16000 20 with 24 KB (1008 workgroups), 26 with 12 or with 48 (512).  Masks:
+  // 128 x 7 rows of 151936 121 us with 56 KB, 132 with 28 or 112.  Neither: 8 x 3 behind 4096
+  // 8.9 us with 600 workgroups, 10.1 with 304 or 1192.
+  const int64_t want = s.logits != s.out ? 20 << 10 : s.mask != nullptr ? 40 << 10 : INT64_MAX;
   int T = kShapeMinTokens;
-  while (T < kShapeMaxTokens && (long long)s.B * ((s.V + T - 1) / T) > most) T *= 2;
+  while (T < kShapeMaxTokens && ((s.R * T * (int64_t)el < want && workgroups(2 * T) > 2ll * cus) ||
+                                 !fits(workgroups(T), kShapeThreads)))
+    T *= 2;
   A.lgT = __builtin_ctz((unsigned)T);
   A.parts = (s.V + T - 1) / T;
-  const long long grid = (long long)s.B * A.parts;
+  const long long grid = workgroups(T);
   const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T) : ShapeLds<4>::bytes(T);
   return s.dtype == ASYMSPEC_BF16 ? shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, stream)
                                   : shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, stream);
