@@ -294,6 +294,7 @@ def test_draw_of_many_tokens(N, V):
     rng = np.random.default_rng(N)
     g = torch.Generator(device="cuda").manual_seed(N)
     x = (torch.randn(N, V, generator=g, device="cuda") * 3).to(torch.bfloat16)
+    x[0] = 0.0
     x[1, 1024 * 3 + 7] = 0.0
     x[2, 5000 - 900:5000] = -math.inf
     x[3 % N, ::3] = -math.inf
