@@ -39,43 +39,49 @@ struct SlotsReq {
   uint32_t need;          // blocks
   int held, fresh;        // blocks held; new tokens
 };
-STEP_DEV SlotsReq slots_req(const SlotsArgs& A, int b) {
-  const int given = A.new_tokens ? A.new_tokens[b] : A.width, len = A.lengths[b], held = A.n_blocks[b];
-  const bool gone = A.release && A.release[b] != 0;
+STEP_DEV SlotsReq slots_req(const SlotsArgs& A, int given, int len, int held, int release) {
   int n = max(given, 0);
   if (A.width > 0) n = min(n, A.width);
   const uint32_t end = (uint32_t)max(len, 0) + (uint32_t)n, bs = (uint32_t)A.block_size, full = end / bs;
   SlotsReq q;
-  q.fresh = gone ? 0 : n;
-  q.need = gone ? 0u : full + (end != full * bs ? 1u : 0u);
+  q.fresh = release != 0 ? 0 : n;
+  q.need = release != 0 ? 0u : full + (end != full * bs ? 1u : 0u);
   q.held = min(max(held, 0), A.max_blocks);
   return q;
 }
 
-// Exclusive sums of three values over the workgroup's threads, in their order.
-STEP_DEV void slots_scan(int64_t (&v)[3], int64_t (*lds)[3]) {
+// Sums below 2^32, or 2^32 - 1.
+STEP_DEV uint32_t slots_add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROWMASK = 0xF>
+STEP_DEV uint32_t slots_dpp(uint32_t x) {     // 0 where a lane has no source
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWMASK, 0xF, false);
+}
+// Exclusive sums of N values over the workgroup's threads, in their order.
+template <int N>
+STEP_DEV void slots_scan(uint32_t (&v)[N], uint32_t (*lds)[3]) {
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-  int64_t up[3];
+  uint32_t up[N];
 #pragma unroll
-  for (int k = 0; k < 3; ++k) up[k] = v[k];
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const int64_t o = __shfl_up(up[k], off, 64);
-      if (lane >= off) up[k] += o;
-    }
+  for (int k = 0; k < N; ++k) {
+    uint32_t x = v[k];
+    x = slots_add(x, slots_dpp<0x111>(x));
+    x = slots_add(x, slots_dpp<0x112>(x));
+    x = slots_add(x, slots_dpp<0x114>(x));
+    x = slots_add(x, slots_dpp<0x118>(x));
+    x = slots_add(x, slots_dpp<0x142, 0xA>(x));
+    up[k] = slots_add(x, slots_dpp<0x143, 0xC>(x));
+    v[k] = slots_dpp<0x138>(up[k]);
   }
   __syncthreads();
   if (lane == 63) {
 #pragma unroll
-    for (int k = 0; k < 3; ++k) lds[wave][k] = up[k];
+    for (int k = 0; k < N; ++k) lds[wave][k] = up[k];
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    for (int w = 0; w < wave; ++w) up[k] += lds[w][k];
-    v[k] = up[k] - v[k];
+  for (int k = 0; k < N; ++k) {
+#pragma unroll
+    for (int w = 0; w < kSlotsThreads / 64; ++w) v[k] = slots_add(v[k], w < wave ? lds[w][k] : 0u);
   }
 }
 
@@ -92,7 +98,7 @@ STEP_DEV int slots_find(const int* from, int B, int i) {
 
 __global__ __launch_bounds__(kSlotsThreads) void slots_kernel(SlotsArgs A) {
   extern __shared__ int slots_lds[];
-  __shared__ int64_t sums[kSlotsThreads / 64][3];
+  __shared__ uint32_t sums[kSlotsThreads / 64][3];
   const int tid = (int)threadIdx.x, B = A.B, N = A.ring_size;
   int* taken = slots_lds;                   // [B + 1] blocks taken ahead of a request
   int* given = slots_lds + B + 1;           // [B + 1] blocks given back ahead of it
@@ -104,44 +110,69 @@ __global__ __launch_bounds__(kSlotsThreads) void slots_kernel(SlotsArgs A) {
   if (head < 0) head += N;
 
   // each thread scans a run of requests: what all ask for decides who is short,
-  // and what the others take and give is scanned again
+  // and what the others take and give is scanned again.  Blocks are below 2^31
+  // (B * max_blocks), new tokens may add up to more.
   const int per = (B + kSlotsThreads - 1) / kSlotsThreads;
   const int lo = min(B, tid * per), hi = min(B, lo + per);
-  int64_t v[3] = {0, 0, 0};
-  for (int b = lo; b < hi; ++b) {
-    const SlotsReq q = slots_req(A, b);
-    delta[b] = q.need <= (uint32_t)A.max_blocks ? (int)q.need - q.held : kShort;
-    start[b] = q.fresh;
-    if (delta[b] > 0) v[0] += delta[b];
+  uint32_t ask[1] = {0u};
+  constexpr int kAhead = 4;             // requests whose values are on their way together
+  for (int b0 = lo; b0 < hi; b0 += kAhead) {
+    int len[kAhead], held[kAhead], given[kAhead], release[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int b = min(b0 + u, hi - 1);
+      len[u] = A.lengths[b];
+      held[u] = A.n_blocks[b];
+      given[u] = A.width;
+      release[u] = 0;
+    }
+    if (A.new_tokens) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) given[u] = A.new_tokens[min(b0 + u, hi - 1)];
+    }
+    if (A.release) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) release[u] = A.release[min(b0 + u, hi - 1)];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (b0 + u < hi) {
+        const SlotsReq q = slots_req(A, given[u], len[u], held[u], release[u]);
+        const int d = q.need <= (uint32_t)A.max_blocks ? (int)q.need - q.held : kShort;
+        delta[b0 + u] = d;
+        start[b0 + u] = q.fresh;
+        if (d > 0) ask[0] += (uint32_t)d;
+      }
+    }
   }
-  slots_scan(v, sums);
-  int64_t asked = v[0];
-  v[0] = v[1] = v[2] = 0;
+  slots_scan(ask, sums);
+  uint32_t asked = ask[0], v[3] = {0u, 0u, 0u};
   for (int b = lo; b < hi; ++b) {
     const int d = delta[b];
     if (d > 0) {
-      asked += d;
-      if (asked > count) delta[b] = kShort;
-      else v[0] += d;
+      asked += (uint32_t)d;
+      if (asked > (uint32_t)count) delta[b] = kShort;
+      else v[0] += (uint32_t)d;
     } else if (d != kShort) {
-      v[1] -= d;
+      v[1] += (uint32_t)-d;
     }
-    v[2] += start[b];
+    v[2] = slots_add(v[2], (uint32_t)start[b]);
   }
   slots_scan(v, sums);
+  auto most = [](uint32_t x) { return (int)min(x, 0x7FFFFFFFu); };
   for (int b = lo; b < hi; ++b) {
     const int d = delta[b], fresh = start[b];
     taken[b] = (int)v[0];
     given[b] = (int)v[1];
-    start[b] = (int)min(v[2], (int64_t)0x7FFFFFFF);
-    if (d > 0) v[0] += d;
-    else if (d != kShort) v[1] -= d;
-    v[2] += fresh;
+    start[b] = most(v[2]);
+    if (d > 0) v[0] += (uint32_t)d;
+    else if (d != kShort) v[1] += (uint32_t)-d;
+    v[2] = slots_add(v[2], (uint32_t)fresh);
   }
   if (lo < hi && hi == B) {
     taken[B] = (int)v[0];
     given[B] = (int)v[1];
-    start[B] = (int)min(v[2], (int64_t)0x7FFFFFFF);
+    start[B] = most(v[2]);
   }
   __syncthreads();
 
