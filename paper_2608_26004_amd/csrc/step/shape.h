@@ -59,7 +59,7 @@ struct ShapeArgs {
   int lgT, parts;    // log2 of a workgroup's tokens, workgroups of a request
 };
 
-// LDS of a workgroup, ahead of the words [T].
+// LDS of a workgroup, ahead of the words [T] and the bias values [n_bias].
 template <int VE>
 struct ShapeLds {
   static constexpr int kGroups = kShapeMaxTokens / VE;
@@ -68,21 +68,27 @@ struct ShapeLds {
   int mask_row[ASYMSPEC_SHAPE_MAX_ROWS];        // -1: no mask
   unsigned long long has_word[kGroups / 64];    // bit g % 64 of g / 64: vector g is listed
   uint16_t list[kGroups];
-  static size_t bytes(int T) { return sizeof(ShapeLds) + (size_t)T * 4; }
+  static size_t bytes(int T, int n_bias) { return sizeof(ShapeLds) + ((size_t)T + n_bias) * 4; }
 };
 static_assert(sizeof(ShapeLds<8>) % 16 == 0 && sizeof(ShapeLds<4>) % 16 == 0, "the words follow, aligned");
 
 struct ShapeCtx {
   float rep, freq, pres;
-  const float* bias;        // the request's bias values
+  const float* bias;        // the request's bias values, of the entries here, in LDS
   const int* drafts;        // in LDS
 };
+typedef int i4 __attribute__((ext_vector_type(4)));
 
 // One logit with a nonzero word; the first n_drafts drafts precede it.
 STEP_DEV float shape_one(float v, uint32_t w, int token, int n_drafts, const ShapeCtx& c) {
   int cnt = (int)(w & kCount);
-  if (w & kInDrafts)
-    for (int j = 0; j < n_drafts; ++j) cnt += c.drafts[j] == token ? 1 : 0;
+  if (w & kInDrafts) {
+    for (int j = 0; j < n_drafts; j += 4) {
+      const i4 d = *(const i4*)(c.drafts + j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) cnt += d[i] == token && j + i < n_drafts ? 1 : 0;
+    }
+  }
   if (cnt > 0 || (w & kInPrompt)) v = v > 0.0f ? v / c.rep : v * c.rep;
   if (cnt > 0) v = (v - c.freq * (float)cnt) - c.pres;
   if (w >> kBiasShift) v = v + c.bias[(w >> kBiasShift) - 1u];
@@ -109,7 +115,8 @@ __global__ __launch_bounds__(kShapeThreads) __attribute__((amdgpu_waves_per_eu(8
   c.rep = s.repetition ? s.repetition[b] : 1.0f;
   c.freq = s.frequency ? s.frequency[b] : 0.0f;
   c.pres = s.presence ? s.presence[b] : 0.0f;
-  c.bias = s.bias_values ? s.bias_values + (size_t)b * s.n_bias : nullptr;
+  float* biases = (float*)(words + T);
+  c.bias = biases;
   c.drafts = S.drafts;
   // such penalties change no logit, so the lists behind them are not read
   const bool counts = !(c.rep == 1.0f && c.freq == 0.0f && c.pres == 0.0f);
@@ -137,11 +144,15 @@ __global__ __launch_bounds__(kShapeThreads) __attribute__((amdgpu_waves_per_eu(8
   if (h) fetch(0);
   constexpr int kBias = (ASYMSPEC_SHAPE_MAX_BIAS + kShapeThreads - 1) / kShapeThreads;
   uint32_t bias_id[kBias];
+  float bias[kBias];
   if (s.n_bias > 0) {
 #pragma unroll
-    for (int k = 0; k < kBias; ++k)
-      bias_id[k] = tid + k * kShapeThreads < s.n_bias
-                       ? (uint32_t)s.bias_ids[(size_t)b * s.n_bias + tid + k * kShapeThreads] : ~0u;
+    for (int k = 0; k < kBias; ++k) {
+      const int i = tid + k * kShapeThreads;
+      const size_t at = (size_t)b * s.n_bias + i;
+      bias_id[k] = i < s.n_bias ? (uint32_t)s.bias_ids[at] : ~0u;
+      bias[k] = i < s.n_bias ? s.bias_values[at] : 0.0f;
+    }
   }
   uint32_t draft = ~0u;
   if (counts && tid < s.D) draft = (uint32_t)s.draft_tokens[b * s.draft_stride + tid];
@@ -165,7 +176,10 @@ __global__ __launch_bounds__(kShapeThreads) __attribute__((amdgpu_waves_per_eu(8
 #pragma unroll
     for (int k = 0; k < kBias; ++k) {
       const uint32_t x = bias_id[k] - (uint32_t)x0;
-      if (x < (uint32_t)n) atomicMax(&words[x], (uint32_t)(tid + k * kShapeThreads + 1) << kBiasShift);
+      if (x < (uint32_t)n) {
+        atomicMax(&words[x], (uint32_t)(tid + k * kShapeThreads + 1) << kBiasShift);
+        biases[tid + k * kShapeThreads] = bias[k];
+      }
     }
     __syncthreads();
   }

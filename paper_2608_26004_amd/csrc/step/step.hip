@@ -169,7 +169,7 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   A.lgT = __builtin_ctz((unsigned)T);
   A.parts = (s.V + T - 1) / T;
   const long long grid = workgroups(T);
-  const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T) : ShapeLds<4>::bytes(T);
+  const size_t lds = s.dtype == ASYMSPEC_BF16 ? ShapeLds<8>::bytes(T, s.n_bias) : ShapeLds<4>::bytes(T, s.n_bias);
   return s.dtype == ASYMSPEC_BF16 ? shape_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, stream)
                                   : shape_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, stream);
 }
