@@ -79,19 +79,25 @@ struct ShapeCtx {
 };
 typedef int i4 __attribute__((ext_vector_type(4)));
 
-// One logit with a nonzero word; the first n_drafts drafts precede it.
-STEP_DEV float shape_one(float v, uint32_t w, int token, int n_drafts, const ShapeCtx& c) {
+// One logit behind its word (0: as it was); the first n_drafts drafts precede it.  All
+// lanes go the same way: of 64 vectors with a word nearly every place has one in some lane.
+STEP_DEV float shape_one(float l, uint32_t w, int token, int n_drafts, const ShapeCtx& c) {
   int cnt = (int)(w & kCount);
-  if (w & kInDrafts) {
+  if (__any((w & kInDrafts) != 0u)) {
+    const bool mine = (w & kInDrafts) != 0u;
     for (int j = 0; j < n_drafts; j += 4) {
       const i4 d = *(const i4*)(c.drafts + j);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) cnt += d[i] == token && j + i < n_drafts ? 1 : 0;
+      for (int i = 0; i < 4; ++i) cnt += mine && d[i] == token && j + i < n_drafts ? 1 : 0;
     }
   }
-  if (cnt > 0 || (w & kInPrompt)) v = v > 0.0f ? v / c.rep : v * c.rep;
-  if (cnt > 0) v = (v - c.freq * (float)cnt) - c.pres;
-  if (w >> kBiasShift) v = v + c.bias[(w >> kBiasShift) - 1u];
+  float v = l > 0.0f ? l / c.rep : l * c.rep;
+  v = cnt > 0 || (w & kInPrompt) ? v : l;
+  v = cnt > 0 ? (v - c.freq * (float)cnt) - c.pres : v;
+  if (__any((w >> kBiasShift) != 0u)) {
+    const float bias = c.bias[max((int)(w >> kBiasShift) - 1, 0)];
+    v = (w >> kBiasShift) ? v + bias : v;
+  }
   return v;
 }
 
@@ -253,12 +259,9 @@ __global__ __launch_bounds__(kShapeThreads) __attribute__((amdgpu_waves_per_eu(8
     const int nd = s.D ? d0 + r : 0;
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-      const uint32_t w = words[g * VE + e];
-      if (w != 0u) {
-        // (ahead of its drafts a token is as it was, whatever bits it has)
-        const float l = Row<DT>::get(v, e), f = shape_one(l, w, x0 + (int)g * VE + e, nd, c);
-        if (__float_as_uint(f) != __float_as_uint(l)) Row<DT>::put(v, e, f);
-      }
+      // (ahead of its drafts a token is as it was, whatever bits it has)
+      const float l = Row<DT>::get(v, e), f = shape_one(l, words[g * VE + e], x0 + (int)g * VE + e, nd, c);
+      if (__float_as_uint(f) != __float_as_uint(l)) Row<DT>::put(v, e, f);
     }
   };
   // A few rows at a time: as many as give each wave its vectors in flight.
