@@ -535,6 +535,45 @@ def test_captured_steps_replay():
             assert torch.equal(a, b)
 
 
+def test_captured_large_draw_and_masked_copy_replay():
+    """The draw through a table and a masked copy, captured; replayed on new inputs
+    with eager calls of the same between the replays."""
+    B, R, V, N = 40, 3, 20011, 300
+
+    def state(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        x = (torch.randn(N, V, generator=g, device="cuda") * 3).to(torch.bfloat16)
+        mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (4, (V + 31) // 32), generator=g, device="cuda", dtype=torch.int64)
+        return [x, gpu(rng.choice(np.float32([0, 0.7, 1]), N)), gpu(rng.random(N, dtype=np.float32)), mask.int(),
+                gpu(i32(rng.integers(-1, 4, (B, R)))), gpu(i32(rng.integers(0, V, (B, 50)))),
+                gpu(i32(rng.integers(0, 51, B))), gpu((1 + rng.random(B)).astype(np.float32))]
+
+    def call(x, tau, u, mask, index, hist, lens, rep):
+        rows = x[:B * R].view(B, R, V)
+        out = torch.empty_like(rows)
+        asp.shape_logits(rows, history=hist, lengths=lens, repetition=rep, mask=mask, mask_index=index, out=out)
+        return (out.view(torch.int16), *asp.draw_tokens(x, tau, u))
+
+    static = state(0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call(*static)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = call(*static)
+    for seed in range(1, 5):
+        fresh = state(seed)
+        for a, b in zip(static, fresh):
+            a.copy_(b)
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, call(*fresh)):
+            assert torch.equal(a, b)
+
+
 def test_calls_on_two_streams_at_once():
     """Two streams, each with its own state, a dozen steps each enqueued in turn."""
     torch.cuda.synchronize()
