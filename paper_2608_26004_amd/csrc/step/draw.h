@@ -38,7 +38,7 @@ constexpr int kDrawChunk = 64 * kDrawPer;     // tokens of a chunk
 
 struct DrawPart {
   double sum;      // of the chunk's weights; 0 without any
-  float m;         // the chunk's largest logit
+  float m;         // the chunk's largest logit; 0 where its weights are 2^(k l), -inf without any
   int32_t arg;     // greedy rows: its first index in the row; else kPlain where the
                    // weights are 2^(k l - rint(k m)), and 0 where 2^(k (l - m))
 };
