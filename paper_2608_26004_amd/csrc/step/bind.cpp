@@ -128,7 +128,7 @@ void* stream_of(PyObject* o) {
 struct Outs {
   PyObject* tuple;
   Tensor own[5];
-  const Tensor* at[5];
+  const Tensor* at[5] = {};         // (new ones of an empty batch are not made: the entry points refuse it)
   size_t offset[5];
   at::ScalarType type[5];
   int64_t shape[5][2];

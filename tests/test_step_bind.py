@@ -1,0 +1,45 @@
+"""The Python binding of the operators around the decision step, on the CPU:
+what it refuses, which the C entry points do not see, and what it leaves to
+them.  Tensors that claim a device without having memory there (fake tensors)
+go through its checks as those of a GPU do."""
+
+import warnings
+
+import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+import paper_2608_26004_amd as asp
+from paper_2608_26004_amd import step
+
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="host-only check")
+
+
+@pytest.fixture(autouse=True)
+def no_stream(monkeypatch):
+    """(without a GPU there is no current stream to ask for)"""
+    monkeypatch.setattr(step, "_raw_stream", lambda device: 0)
+
+
+def fake(make):
+    """The tensors that `make` makes, on a GPU that is not there."""
+    with warnings.catch_warnings():
+        warnings.simplefilter("ignore")
+        with FakeTensorMode():
+            return make(lambda *s: torch.empty(*s, dtype=torch.int32, device="cuda"),
+                        lambda *s: torch.empty(*s, device="cuda"))
+
+
+EMPTY = {
+    "shape_logits": lambda i, f: (f(0, 3, 64),),
+    "draw_tokens": lambda i, f: (f(0, 64), f(0), f(0)),
+    "commit_tokens": lambda i, f: (i(0), i(0), i(0, 2), i(0, 9), i(0)),
+    "plan_slots": lambda i, f: (i(0), None, i(0, 4), i(0), i(8), i(2), 16, 3),
+}
+
+
+@pytest.mark.parametrize("name", sorted(EMPTY))
+def test_an_empty_batch_is_refused(name):
+    with pytest.raises(asp.AsymSpecError) as e:
+        getattr(asp, name)(*fake(EMPTY[name]))
+    assert e.value.status == asp.E_ARG
