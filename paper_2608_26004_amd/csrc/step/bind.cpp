@@ -128,7 +128,7 @@ void* stream_of(PyObject* o) {
 struct Outs {
   PyObject* tuple;
   Tensor own[5];
-  const Tensor* at[5] = {};         // (new ones of an empty batch are not made: the entry points refuse it)
+  const Tensor* at[5] = {};
   size_t offset[5];
   at::ScalarType type[5];
   int64_t shape[5][2];
@@ -360,7 +360,7 @@ PyObject* commit_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Device dev = h.device();
     const Tensor* stops = tensor("stop_tokens", a[6]);
     const int64_t n_stop = stops != nullptr ? stops->numel() : 0;
-    if (B > kMostInt || K > kMostInt || L > kMostInt || n_stop > kMostInt) check(ASYMSPEC_E_ARG);
+    if (B < 1 || B > kMostInt || K > kMostInt || L > kMostInt || n_stop > kMostInt) check(ASYMSPEC_E_ARG);
     const int* acc = need_as<int>("accept_len", &given("accept_len", a[0]), {B}, dev);
     const int* nxt = need_as<int>("next_token", &given("next_token", a[1]), {B}, dev);
     const int* dp = need_as<int>("draft_tokens", &d, {B, K}, dev, false);
@@ -394,7 +394,7 @@ PyObject* plan_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor &table = given("block_table", a[2]), &ring = given("free_ring", a[4]);
     if (table.dim() != 2 || ring.dim() != 1) refuse("block_table must be [B, max_blocks] and free_ring [pool]");
     const int64_t B = table.size(0), top = table.size(1), N = ring.size(0);
-    if (B > kMostInt || top > kMostInt || N > kMostInt) check(ASYMSPEC_E_ARG);
+    if (B < 1 || B > kMostInt || top > kMostInt || N > kMostInt) check(ASYMSPEC_E_ARG);
     const int64_t bs = number("block_size", a[6], 1, kMostInt);
     const int64_t width = number("width", a[7], 0, kMostInt), total = number("total", a[8], 0, kMostInt);
     const Tensor* fresh_tokens = tensor("new_tokens", a[1]);
