@@ -280,8 +280,9 @@ PyObject* shape_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (D == 0) s.draft_tokens = nullptr;
     if (n_bias == 0) s.bias_ids = nullptr, s.bias_values = nullptr;
     if (n_masks == 0) s.mask = nullptr, s.mask_index = nullptr;
-    // an id map of no entries maps nothing: some address, which is not read
-    if (id_map != nullptr && n_ids == 0) s.id_map = (const int32_t*)x.data_ptr();
+    // an id map of no entries maps nothing: an address that is aligned, and not read
+    static const int32_t kNoIds = 0;
+    if (id_map != nullptr && n_ids == 0) s.id_map = &kNoIds;
     s.B = (int)B;
     s.R = (int)R;
     s.V = (int)V;

@@ -27,7 +27,7 @@ def fake(make):
         warnings.simplefilter("ignore")
         with FakeTensorMode():
             return make(lambda *s: torch.empty(*s, dtype=torch.int32, device="cuda"),
-                        lambda *s: torch.empty(*s, device="cuda"))
+                        lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device="cuda"))
 
 
 EMPTY = {
@@ -43,3 +43,13 @@ def test_an_empty_batch_is_refused(name):
     with pytest.raises(asp.AsymSpecError) as e:
         getattr(asp, name)(*fake(EMPTY[name]))
     assert e.value.status == asp.E_ARG
+
+
+@pytest.mark.parametrize("offset", [2, 3])
+def test_an_empty_id_map_beside_logits_of_any_alignment(offset):
+    """It maps nothing, wherever the bf16 rows begin: the call is valid and ends at
+    the device, which is missing here."""
+    x, ids = fake(lambda i, f: (f(2, 3, 80, dtype=torch.bfloat16)[..., offset:offset + 64], i(0)))
+    with pytest.raises(asp.AsymSpecError) as e:
+        asp.shape_logits(x, id_map=ids)
+    assert e.value.status == asp.E_DEVICE
