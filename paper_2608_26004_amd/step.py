@@ -40,7 +40,7 @@ def _bind():
 
 
 def _stream(x):
-    i = x.get_device()
+    i = x.get_device() if isinstance(x, torch.Tensor) else -1      # (the binding refuses what is none)
     return _raw_stream(i) if i >= 0 else 0
 
 

@@ -53,3 +53,20 @@ def test_an_empty_id_map_beside_logits_of_any_alignment(offset):
     with pytest.raises(asp.AsymSpecError) as e:
         asp.shape_logits(x, id_map=ids)
     assert e.value.status == asp.E_DEVICE
+
+
+def test_what_is_no_tensor_is_refused():
+    """TypeError, wherever it stands among the arguments."""
+    i, f = (lambda *s: torch.zeros(*s, dtype=torch.int32)), torch.zeros
+    commit, slots = [i(2), i(2), i(2, 3), i(2, 9), i(2)], [i(2), i(2), i(2, 4), i(2), i(8), i(2)]
+    for bad in (None, [1, 2], 3.0):
+        with pytest.raises(TypeError):
+            asp.shape_logits(bad)
+        with pytest.raises(TypeError):
+            asp.draw_tokens(bad, f(2), f(2))
+        for k in range(len(commit)):
+            with pytest.raises(TypeError):
+                asp.commit_tokens(*commit[:k], bad, *commit[k + 1:])
+        for k in (0, 2, 3, 4, 5):
+            with pytest.raises(TypeError):
+                asp.plan_slots(*slots[:k], bad, *slots[k + 1:], 16, width=1)
