@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <hip/hip_runtime_api.h>
@@ -86,6 +87,18 @@ T* need_as(const char* name, const Tensor* t, at::IntArrayRef shape, const at::D
   return (T*)need(name, t, c10::CppTypeToScalarType<T>::value, shape, dev, contiguous);
 }
 
+// Ahead of a call that writes a tensor (null: none): nothing of it is recorded, so one
+// that requires a gradient would get a wrong one.
+void writable(const char* name, const Tensor* t) {
+  if (t != nullptr && t->requires_grad() && c10::GradMode::is_enabled())
+    refuse(std::string(name) + " requires a gradient and would be written to: detach it, or call under torch.no_grad()");
+}
+// Behind it: a new version, as behind every in-place operation, so that a backward pass
+// that saved the tensor says so.  (Inference tensors have no versions.)
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int logit_type(const Tensor& t) {
   if (t.scalar_type() == at::kBFloat16) return ASYMSPEC_BF16;
   if (t.scalar_type() == at::kFloat) return ASYMSPEC_FP32;
@@ -139,7 +152,10 @@ struct Outs {
     if (o == Py_None) return;
     if (!PyTuple_Check(o) && !PyList_Check(o)) refuse("out must be a tuple of tensors", PyExc_TypeError);
     if (PySequence_Fast_GET_SIZE(o) != n) refuse("out must have " + std::to_string(n) + " tensors");
-    for (int i = 0; i < n; ++i) at[i] = &given("out", PySequence_Fast_GET_ITEM(o, i));
+    for (int i = 0; i < n; ++i) {
+      at[i] = &given("out", PySequence_Fast_GET_ITEM(o, i));
+      writable("out", at[i]);
+    }
   }
   bool made() const { return tuple == Py_None; }
   at::IntArrayRef sizes(int i) const { return at::IntArrayRef(shape[i], dims[i]); }
@@ -175,7 +191,10 @@ struct Outs {
   T* ptr(const char* name, int i, const at::Device& dev, bool contiguous = true) const {
     return (T*)need(name, at[i], type[i], sizes(i), dev, contiguous);
   }
+  // (behind the call)
   PyObject* result() {
+    if (!made())
+      for (int i = 0; i < n; ++i) written(*at[i]);
     PyObject* r = PyTuple_New(n);
     if (r == nullptr) throw Raised{};
     for (int i = 0; i < n; ++i) {
@@ -227,6 +246,7 @@ PyObject* shape_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (out.scalar_type() != x.scalar_type() || out.sizes() != x.sizes() || out.device() != dev)
       refuse("out must have the logits' shape, dtype and device");
     if (V > 1 && (x.stride(2) != 1 || out.stride(2) != 1)) refuse("rows of logits must be contiguous");
+    writable(given_out != nullptr ? "out" : "logits", &out);
     const Tensor *history = tensor("history", a[1]), *lengths = tensor("lengths", a[2]),
                  *prompt = tensor("prompt_lengths", a[3]), *drafts = tensor("draft_tokens", a[4]),
                  *bias_ids = tensor("bias_ids", a[8]), *bias_values = tensor("bias_values", a[9]),
@@ -295,6 +315,7 @@ PyObject* shape_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     s.out = out.data_ptr();
     const OnDevice on(dev);
     check(asymspec_shape_logits(&s, stream_of(a[14])));
+    written(out);
     PyObject* r = a[given_out != nullptr ? 13 : 0];
     Py_INCREF(r);
     return r;
@@ -384,6 +405,7 @@ PyObject* commit_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
     check(asymspec_commit_tokens(acc, nxt, K > 0 ? dp : nullptr, d.stride(0), hp, (int)L, len, fin,
                                  n_stop > 0 ? sp : nullptr, (int)n_stop, most, (int)B, (int)K, lo, fo, to, co,
                                  stream_of(a[9])));
+    written(h);
     return out.result();
   });
 }
@@ -425,6 +447,8 @@ PyObject* plan_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int* starts = width == 0 ? out.ptr<int>("out[4]", 4, dev) : nullptr;
     check(asymspec_plan_slots(len, add, rel, tp, (int)top, held, rp, (int)N, state, (int)bs, (int)B, (int)width,
                               (int)total, slots, starts, is_short, held_out, state_out, stream_of(a[11])));
+    written(table);
+    written(ring);
     return out.result();
   });
 }

@@ -4,7 +4,9 @@
 ``include/asymspec_step.h``; the work is done by the HIP kernels of
 ``csrc/step/`` on the tensors' device and its current stream.  Every tensor is
 on that device; index tensors are int32.  The calls may be captured into a HIP
-graph.  There is no fallback: if a library is missing, every call raises.
+graph.  No gradient passes through them: a tensor that a call writes to must not
+require one (under torch.no_grad() it may), and has a new version afterwards.
+There is no fallback: if a library is missing, every call raises.
 """
 
 from __future__ import annotations

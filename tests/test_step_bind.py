@@ -70,3 +70,22 @@ def test_what_is_no_tensor_is_refused():
         for k in (0, 2, 3, 4, 5):
             with pytest.raises(TypeError):
                 asp.plan_slots(*slots[:k], bad, *slots[k + 1:], 16, width=1)
+
+
+def test_writing_to_a_tensor_that_requires_a_gradient_is_refused():
+    """A gradient through it would be wrong without a word; without gradients, or
+    on a detached one, the call goes on (here to the missing GPU)."""
+    x, y = torch.zeros(2, 3, 64, requires_grad=True), torch.zeros(2, 3, 64)
+    q = torch.zeros(6, requires_grad=True)
+    t = torch.zeros(6, dtype=torch.int32)
+    draw = (y.view(6, 64), torch.ones(6), torch.ones(6))
+    for call in (lambda: asp.shape_logits(x), lambda: asp.shape_logits(x * 2), lambda: asp.shape_logits(y, out=x),
+                 lambda: asp.draw_tokens(*draw, out=(t, q))):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="must be on the GPU"):
+            call()
+    for call in (lambda: asp.shape_logits(x.detach()), lambda: asp.shape_logits(x, out=y),
+                 lambda: asp.draw_tokens(x[0], torch.ones(3), torch.ones(3))):
+        with pytest.raises(ValueError, match="must be on the GPU"):
+            call()

@@ -591,3 +591,50 @@ def test_calls_on_two_streams_at_once():
         for a, b in zip(got[k], want[k]):
             for x, y in zip(a, b):
                 assert torch.equal(x, y)
+
+
+# ------------------------------------------------------------ beside autograd --
+def test_calls_that_write_count_as_in_place():
+    """Every tensor that a call writes has a new version, so that a backward pass
+    that saved it says so; one that is only read, or new, has not."""
+    B, K, V, L = 3, 2, 500, 20
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")     # noqa: E731
+    x, out, one = torch.randn(B, K + 1, V, device="cuda"), torch.empty(B, K + 1, V, device="cuda"), torch.ones(B, device="cuda")
+    hist, lens, d, tok, q = i(B, L), i(B), i(B, K), i(B), torch.empty(B, device="cuda")
+    table, held, ring, state = i(B, 4), i(B), torch.arange(12, dtype=torch.int32, device="cuda"), i(2)
+    commit_out, slots_out = (i(B), i(B), i(B, K + 1), i(B)), (i(B, 1).long(), i(B), i(B), i(2))
+    everything = [x, out, one, hist, lens, d, tok, q, table, held, ring, state, *commit_out, *slots_out]
+
+    def changed(call, want):
+        before = [t._version for t in everything]
+        new = call()
+        assert {id(t) for t, v in zip(everything, before) if t._version > v} == {id(t) for t in want}
+        assert all(t._version == 0 for t in new if not any(t is e for e in everything))
+
+    changed(lambda: [asp.shape_logits(x, presence=one)], [x])
+    changed(lambda: [asp.shape_logits(x, out=out)], [out])
+    changed(lambda: asp.draw_tokens(x[:, 0], one, one), [])
+    changed(lambda: asp.draw_tokens(x[:, 0], one, one, out=(tok, q)), [tok, q])
+    changed(lambda: asp.commit_tokens(lens, tok, d, hist, lens), [hist])
+    changed(lambda: asp.commit_tokens(lens, tok, d, hist, lens, out=commit_out), [hist, *commit_out])
+    changed(lambda: asp.plan_slots(lens, None, table, held, ring, state, 16, width=1), [table, ring])
+    changed(lambda: asp.plan_slots(lens, None, table, held, ring, state, 16, width=1, out=slots_out),
+            [table, ring, *slots_out])
+    w = torch.ones(1, device="cuda", requires_grad=True)
+    y = (w * x).sum()
+    asp.shape_logits(x[:, 1:], presence=one)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
+    with torch.inference_mode():
+        z = torch.zeros(B, 1, V, device="cuda")
+    assert asp.shape_logits(z, presence=one) is z      # a tensor without versions
+
+
+def test_an_empty_id_map_maps_nothing():
+    x, _ = stored(np.random.default_rng(2), (2, 3, 80), "bf16")
+    v = x[..., 3:67]
+    keep = x.clone()
+    ids = torch.zeros(0, dtype=torch.int32, device="cuda")
+    h = torch.ones(2, 9, dtype=torch.int32, device="cuda")
+    asp.shape_logits(v, history=h, lengths=h[:, 0].contiguous() * 9, presence=torch.ones(2, device="cuda"), id_map=ids)
+    assert torch.equal(x, keep)
