@@ -64,7 +64,10 @@ std::string text(at::IntArrayRef s) {
 const Tensor* tensor(const char* name, PyObject* o) {
   if (o == Py_None) return nullptr;
   if (!THPVariable_Check(o)) refuse(std::string(name) + " must be a tensor", PyExc_TypeError);
-  return &THPVariable_Unpack(o);
+  const Tensor& t = THPVariable_Unpack(o);
+  // (torch keeps a sign, or that all is zero, beside the memory of such tensors)
+  if (t.is_neg() || t._is_zerotensor()) refuse(std::string(name) + " is lazily negated or zero: pass its clone()");
+  return &t;
 }
 const Tensor& given(const char* name, PyObject* o) {
   const Tensor* t = tensor(name, o);

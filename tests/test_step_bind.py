@@ -89,3 +89,16 @@ def test_writing_to_a_tensor_that_requires_a_gradient_is_refused():
                  lambda: asp.draw_tokens(x[0], torch.ones(3), torch.ones(3))):
         with pytest.raises(ValueError, match="must be on the GPU"):
             call()
+
+
+def test_lazily_negated_tensors_are_refused():
+    """Their memory holds the values without the sign."""
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)     # noqa: E731
+    x, one, neg = torch.zeros(2, 1, 64), torch.ones(2), torch._neg_view
+    for call in (lambda: asp.shape_logits(neg(x)), lambda: asp.shape_logits(x, out=neg(x.clone())),
+                 lambda: asp.shape_logits(x, presence=neg(one)), lambda: asp.draw_tokens(neg(x[:, 0]), one, one),
+                 lambda: asp.draw_tokens(x[:, 0], neg(one), one), lambda: asp.draw_tokens(x[:, 0], one, neg(one)),
+                 lambda: asp.draw_tokens(x[:, 0], one, one, out=(i(2), neg(one))),
+                 lambda: asp.shape_logits(x, presence=torch._efficientzerotensor(2))):
+        with pytest.raises(ValueError, match="negated"):
+            call()
