@@ -19,6 +19,7 @@
 #include <string>
 
 #include "asymspec_step.h"
+#include "span.h"
 
 namespace {
 
@@ -441,13 +442,22 @@ PyObject* plan_slots(PyObject*, PyObject* const* a, Py_ssize_t n) {
     out.is(at::kInt, B);
     out.is(at::kInt, 2);
     if (width == 0) out.is(at::kInt, B + 1);
+    int64_t* slots = nullptr;
+    int *is_short = nullptr, *held_out = nullptr, *state_out = nullptr, *starts = nullptr;
+    auto addresses = [&]() {
+      slots = out.ptr<int64_t>("out[0]", 0, dev);
+      is_short = out.ptr<int>("out[1]", 1, dev);
+      held_out = out.ptr<int>("out[2]", 2, dev);
+      state_out = out.ptr<int>("out[3]", 3, dev);
+      if (width == 0) starts = out.ptr<int>("out[4]", 4, dev);
+    };
+    if (!out.made()) addresses();
+    if (asym_step::slots_overlap(len, add, rel, tp, (int)top, held, rp, (int)N, state, (int)B, (int)width, (int)total,
+                                 slots, starts, is_short, held_out, state_out))
+      refuse("block_table, free_ring and out are written and must overlap no other tensor of the call");
     const OnDevice on(dev);
     out.make(dev);
-    int64_t* slots = out.ptr<int64_t>("out[0]", 0, dev);
-    int* is_short = out.ptr<int>("out[1]", 1, dev);
-    int* held_out = out.ptr<int>("out[2]", 2, dev);
-    int* state_out = out.ptr<int>("out[3]", 3, dev);
-    int* starts = width == 0 ? out.ptr<int>("out[4]", 4, dev) : nullptr;
+    if (out.made()) addresses();
     check(asymspec_plan_slots(len, add, rel, tp, (int)top, held, rp, (int)N, state, (int)bs, (int)B, (int)width,
                               (int)total, slots, starts, is_short, held_out, state_out, stream_of(a[11])));
     written(table);

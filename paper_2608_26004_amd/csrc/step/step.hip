@@ -13,6 +13,7 @@
 #include "draw.h"
 #include "shape.h"
 #include "slots.h"
+#include "span.h"
 
 namespace asym_step {
 
@@ -265,6 +266,9 @@ int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const
   if (!aligned(slots, 8)) return ASYMSPEC_E_ALIGN;
   const int cus = device_cus();
   if (cus == 0) return ASYMSPEC_E_DEVICE;
+  if (slots_overlap(lengths, new_tokens, release, block_table, max_blocks, n_blocks, free_ring, ring_size, free_state, B,
+                    width, total, slots, starts, short_out, n_blocks_out, free_state_out))
+    return ASYMSPEC_E_ARG;
   SlotsArgs A;
   A.lengths = lengths; A.new_tokens = new_tokens; A.release = release; A.table = block_table;
   A.n_blocks = n_blocks; A.ring = free_ring; A.state = free_state; A.slots = slots; A.starts = starts;

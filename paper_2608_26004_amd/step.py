@@ -123,6 +123,7 @@ def plan_slots(lengths, new_tokens, block_table, n_blocks, free_ring, free_state
     Returns (slots int64, -1 where there is no token; short [B] int32, 1 for a
     request that did not get its blocks, which keeps what it has and has no
     slots; n_blocks [B]; free_state [2]), and with `total` also starts [B + 1].
-    out: the tensors to write, in that order."""
+    out: the tensors to write, in that order.  What is written (block_table and
+    free_ring among it) must overlap no other tensor of the call."""
     return (_step or _bind()).plan_slots(lengths, new_tokens, block_table, n_blocks, free_ring, free_state,
                                          block_size, width or 0, total or 0, release, out, _stream(block_table))

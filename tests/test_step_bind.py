@@ -5,6 +5,7 @@ go through its checks as those of a GPU do."""
 
 import warnings
 
+import numpy as np
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -102,3 +103,46 @@ def test_lazily_negated_tensors_are_refused():
                  lambda: asp.shape_logits(x, presence=torch._efficientzerotensor(2))):
         with pytest.raises(ValueError, match="negated"):
             call()
+
+
+def test_slots_that_overlap_are_refused():
+    """Every workgroup of plan_slots reads all requests while others already write:
+    nothing that is written may overlap another tensor."""
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)     # noqa: E731
+    B, top, N, W = 4, 4, 20, 2
+    names = ["lengths", "new_tokens", "block_table", "n_blocks", "free_ring", "free_state", "release"]
+    outs = ["slots", "short", "held", "state", "starts"]
+
+    def call(packed, **over):
+        a = dict(lengths=i(B), new_tokens=i(B), block_table=i(B, top), n_blocks=i(B), free_ring=i(N), free_state=i(2),
+                 release=i(B), slots=torch.zeros(9 if packed else (B, W), dtype=torch.int64), short=i(B), held=i(B),
+                 state=i(2), starts=i(B + 1))
+        a.update(over)
+        kw = {k: a[k] for k in names}
+        own = {k: v for k, v in over.items() if k in outs}
+        out = [a[k] for k in outs[:5 if packed else 4]] if own else None
+        return lambda: asp.plan_slots(**kw, block_size=16, out=out, **({"total": 9} if packed else {"width": W}))
+
+    room = i(400)
+    at = lambda k, *s: room[k:k + int(np.prod(s))].view(*s)     # noqa: E731
+    big = room.view(torch.int64)
+    for packed in (False, True):
+        bad = [dict(short=at(0, B), release=at(0, B)), dict(short=at(3, B), lengths=at(0, B)),
+               dict(held=at(0, B), n_blocks=at(3, B)), dict(held=at(0, B), new_tokens=at(2, B)),
+               dict(state=at(0, 2), free_state=at(1, 2)), dict(state=at(3, 2), lengths=at(0, B)),
+               dict(block_table=at(0, B, top), free_ring=at(15, N)), dict(block_table=at(0, B, top), n_blocks=at(12, B)),
+               dict(free_ring=at(0, N), free_state=at(18, 2)), dict(short=at(0, B), held=at(1, B)),
+               dict(short=at(0, B), block_table=at(2, B, top)),
+               dict(slots=big[:9] if packed else big[:8].view(B, W), lengths=at(15, B))]
+        if packed:
+            bad += [dict(starts=at(0, B + 1), lengths=at(4, B)), dict(starts=at(0, B + 1), short=at(4, B))]
+        for over in bad:
+            with pytest.raises(ValueError, match="overlap"):
+                call(packed, **over)()
+        # side by side, and inputs that are one tensor
+        for over in (dict(short=at(0, B), held=at(B, B), state=at(2 * B, 2), starts=at(2 * B + 2, B + 1),
+                          lengths=at(4 * B, B), n_blocks=at(5 * B, B)),
+                     dict(lengths=at(0, B), new_tokens=at(0, B), release=at(0, B), n_blocks=at(0, B)),
+                     dict(block_table=at(0, B, top), free_ring=at(B * top, N))):
+            with pytest.raises(ValueError, match="must be on the GPU"):
+                call(packed, **over)()

@@ -638,3 +638,25 @@ def test_an_empty_id_map_maps_nothing():
     h = torch.ones(2, 9, dtype=torch.int32, device="cuda")
     asp.shape_logits(v, history=h, lengths=h[:, 0].contiguous() * 9, presence=torch.ones(2, device="cuda"), id_map=ids)
     assert torch.equal(x, keep)
+
+
+def test_slots_overlaps_are_refused_by_the_c_entry():
+    """(enqueues nothing: the ring, the table and the outputs keep their values)"""
+    from test_step_abi import library
+    B, top, N = 4, 4, 20
+    room = torch.arange(400, dtype=torch.int32, device="cuda")
+    keep, p0 = room.clone(), room.data_ptr()
+    place = dict(lens=0, new=4, rel=8, table=16, held=32, ring=40, state=60, slots=64, starts=80, short=88, held_out=92,
+                 state_out=96)
+
+    def call(**over):
+        p = {k: p0 + 4 * v for k, v in {**place, **over}.items()}
+        return library().asymspec_plan_slots(p["lens"], p["new"], p["rel"], p["table"], top, p["held"], p["ring"], N,
+                                             p["state"], 16, B, 2, 0, p["slots"], p["starts"], p["short"], p["held_out"],
+                                             p["state_out"], None)
+
+    for over in (dict(short=8), dict(short=3), dict(held_out=1), dict(held_out=29), dict(state_out=59), dict(starts=0),
+                 dict(slots=14), dict(slots=86), dict(ring=31), dict(table=50), dict(state=59), dict(short=90)):
+        assert call(**over) == asp.E_ARG, over
+    torch.cuda.synchronize()
+    assert torch.equal(room, keep)
