@@ -38,11 +38,11 @@ constexpr int kDrawChunk = 64 * kDrawPer;     // tokens of a chunk
 
 struct DrawPart {
   double sum;      // of the chunk's weights; 0 without any
-  float m;         // the chunk's largest logit; 0 where its weights are 2^(k l), -inf without any
-  int32_t arg;     // greedy rows: its first index in the row; else kPlain where the
-                   // weights are 2^(k l - rint(k m)), and 0 where 2^(k (l - m))
+  float m;         // the chunk's largest logit; -inf without any
+  int32_t arg;     // greedy rows: its first index in the row; else kPlain where the weights
+                   // are 2^(k l - rint(k m)), kTabled where 2^(k l), and 0 where 2^(k (l - m))
 };
-constexpr int32_t kPlain = 1;
+constexpr int32_t kPlain = 1, kTabled = 2;
 
 struct DrawArgs {
   const void* logits;
@@ -104,9 +104,10 @@ struct DrawScale {
   }
   // the weight of a chunk's sum
   STEP_DEV double of_part(const DrawPart& q) const {
-    if (q.arg != kPlain || inf) return weight((double)(inf ? flat(q.m) : q.m));
-    // 2^(rint(k q.m) - k m)
-    const double d = __builtin_fmax(__builtin_fma(-k, m, __builtin_rint(k * (double)q.m)), -2200.0);
+    if ((q.arg != kPlain && q.arg != kTabled) || inf) return weight((double)(inf ? flat(q.m) : q.m));
+    // 2^(rint(k q.m) - k m), or 2^(-k m)
+    const double at = q.arg == kPlain ? __builtin_rint(k * (double)q.m) : 0.0;
+    const double d = __builtin_fmax(__builtin_fma(-k, m, at), -2200.0);
     const double n = __builtin_rint(d), f = d - n;
     double p = __builtin_fma(c[9], f, c[8]);
 #pragma unroll
@@ -285,6 +286,20 @@ constexpr float kTableTau = 0x1p-5f;                              // under it |l
 // 2048 rows of 17 chunks 34.0 and 33.0).
 constexpr int kTableChunks = 20;
 typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+typedef int16_t s2 __attribute__((ext_vector_type(2)));
+
+// The largest logit of a chunk without a not-a-number, from each lane's largest bits as
+// integers with a sign: if none is positive, the least bits are the largest logit's.
+STEP_DEV float draw_top(const u4 (&v)[2], s2 hi) {
+  int top = draw_max_i(max((int)hi[0], (int)hi[1]));
+  if (top < 0) {
+    s2 lo = hi;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lo = __builtin_elementwise_min(lo, __builtin_bit_cast(s2, (uint32_t)v[i / 4][i % 4]));
+    top = ~draw_max_i(max(~(int)lo[0], ~(int)lo[1]));
+  }
+  return __uint_as_float((uint32_t)top << 16);
+}
 
 __global__ __launch_bounds__(kTableThreads) __attribute__((amdgpu_waves_per_eu(8))) void draw_table_kernel(DrawArgs A) {
   constexpr int DT = ASYMSPEC_BF16, VE = 8, NV = kDrawPer / VE, kWaves = kTableThreads / 64;
@@ -313,10 +328,12 @@ __global__ __launch_bounds__(kTableThreads) __attribute__((amdgpu_waves_per_eu(8
     for (int c = c0 + wave; c < c1; c += kWaves, bit <<= 1) {
       if (c + kWaves < c1) draw_load<DT>(p, (c + kWaves) * kDrawChunk, A.V, lane, 64, next);
       h2 at[kDrawPer / 2], most = {0, 0};
+      s2 hi = {-0x8000, -0x8000};
 #pragma unroll
       for (int i = 0; i < kDrawPer / 2; ++i) {
         const uint32_t two = v[i / 4][i % 4];
         const h2 w = __builtin_bit_cast(h2, two);
+        hi = __builtin_elementwise_max(hi, __builtin_bit_cast(s2, two));
         at[i] = (w - (uint16_t)kTableLow) * (uint16_t)2 + (w >> (uint16_t)15);
         most = __builtin_elementwise_max(most, at[i]);
       }
@@ -361,7 +378,8 @@ __global__ __launch_bounds__(kTableThreads) __attribute__((amdgpu_waves_per_eu(8
         }
       } else {
         const double sum = draw_sum_d(part[0]);
-        if (lane == 63) out[c] = DrawPart{sum, sum > 0.0 ? 0.0f : -__builtin_huge_valf(), kPlain};
+        const float top = draw_top(v, hi);
+        if (lane == 63) out[c] = DrawPart{sum, top, kTabled};
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) v[i] = next[i];

@@ -313,6 +313,37 @@ def test_draw_of_many_tokens(N, V):
         assert tok[n] == t1[0] and abs(q[n] - q1[0]) <= 2.0 ** -23 * q1[0]
 
 
+def test_draw_of_the_longest_rows():
+    """2^26 tokens of equal logits whose weights are near the largest that a table
+    holds: their sum is not beyond fp64."""
+    V, u = (1 << 26) + 12345, np.float32(0.3)
+    x = torch.full((1, V), 21.625, dtype=torch.bfloat16, device="cuda")
+    tok, q = asp.draw_tokens(x, gpu(np.float32([2.0 ** -5])), gpu(u[None]))
+    # the first i with i + 1 > u V, which lies half a token from a step
+    assert tok[0] == math.floor(float(u) * V) and q[0].item() == np.float32(1.0 / V)
+
+
+def test_draw_ends_of_the_distribution():
+    """Uniforms of 0 and 1 give the first and the last token with weight: one as far
+    below the row's largest as fp64's exp gives it, whatever its chunk or the row's
+    level; bf16 rows of many tokens."""
+    N, V, tau = 300, 40000, 2.0 ** -5
+    rng = np.random.default_rng(5)
+    x, _ = stored(rng, (N, V), "bf16", 0.5)
+    x[:4, :] = 0.5                          # far below 15: weight of 1e-201; at -15: none
+    x[:4, 20000] = 15.0
+    x[:2, :3000], x[:2, 39000:] = -15.0, -15.0
+    x[2:4, 0:5], x[2:4, V - 7:] = -15.0, -15.0
+    x[4:8, :5000], x[4:8, 35000:] = -40.0, -40.0      # 1e-264 of what -21 weighs
+    x[4:8, 5000:35000] = -21.0
+    x[6:8, 30:2000], x[6:8, V - 100:] = -math.inf, -60.0
+    t = np.full(N, tau, np.float32)
+    u = rng.random(N, dtype=np.float32)
+    u[:8] = [0, 1] * 4
+    tok, _ = check_draw(x, t, u)
+    assert tok[:8].tolist() == [3000, 38999, 5, V - 8, 0, V - 1, 0, V - 101]
+
+
 def test_draw_every_kind_of_not_a_number():
     """Quiet and signalling ones of either sign, as bf16 bit patterns."""
     V = 5000
