@@ -104,10 +104,11 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream);
  *     the first token whose inclusive sum of w exceeds uniforms[n] times the
  *     row's sum, and prob = w(token) / sum: an inverse-CDF draw from
  *     softmax(l / temperature), as the drafter makes it for fuse_verify.
- * Logits of -inf or not a number have no weight; logits of +inf share all of
- * it.  A row without any weight gives token 0 with prob 0.  Uniforms are in
- * [0, 1); below (or not a number) count as 0, at or above 1 give the last
- * token with weight.  The same inputs give the same outputs, bit for bit.
+ * Logits of -inf or not a number have no weight, as has one whose w(x) would be
+ * below fp64's smallest number, 2^-1074; logits of +inf share all of it.  A row
+ * without any weight gives token 0 with prob 0.  Uniforms are in [0, 1); below
+ * (or not a number) count as 0, at or above 1 give the last token with weight.
+ * The same inputs give the same outputs, bit for bit.
  *   logits       (dtype), aligned to an element
  *   uniforms     [N], entries uniform_stride elements apart (may be NULL when
  *                no temperature is positive: then a draw takes 0)

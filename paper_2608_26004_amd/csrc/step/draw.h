@@ -102,7 +102,7 @@ struct DrawScale {
     for (int i = 7; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
     return __builtin_ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, s));
   }
-  // the weight of a chunk's sum
+  // what a chunk's sum is to be multiplied with
   STEP_DEV double of_part(const DrawPart& q) const {
     if ((q.arg != kPlain && q.arg != kTabled) || inf) return weight((double)(inf ? flat(q.m) : q.m));
     // 2^(rint(k q.m) - k m), or 2^(-k m)
@@ -446,7 +446,11 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
     return;
   }
   const DrawScale k(tau, m);
-  auto weight_of = [&](const DrawPart& q) { return q.sum * k.of_part(q); };
+  // A chunk counts if its largest logit has a weight of 2^-1074, fp64's smallest number,
+  // or more: below that a chunk's sum can come out as more than nothing where none of its
+  // tokens has any weight.
+  const float least_m = k.inf ? inf : (float)(k.m + k.least * (744.4400719213812 / 762.0));
+  auto weight_of = [&](const DrawPart& q) { return q.m >= least_m ? q.sum * k.of_part(q) : 0.0; };
   double mine = 0.0, upto, ahead;
   each([&](int, DrawPart& q) {
     const double w = weight_of(q);

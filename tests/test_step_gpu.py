@@ -344,6 +344,22 @@ def test_draw_ends_of_the_distribution():
     assert tok[:8].tolist() == [3000, 38999, 5, V - 8, 0, V - 1, 0, V - 101]
 
 
+@pytest.mark.parametrize("dtype,N,low,top,tau", [
+    # one token of 2^-1075.2, rounded to nothing, but its chunk's sum is not when it is
+    # multiplied out: 2^-1074.7 for the chunk's scale, times 1024 tokens
+    ("fp32", 3, -745.475, -0.20794415, 1.0),
+    # the same through the table: tokens of 2^-1079.1, 2^-1069.1 for the chunk
+    ("bf16", 300, -8.375, 15.0, 2.0 ** -5)])
+def test_draw_of_a_chunk_whose_tokens_have_no_weight(dtype, N, low, top, tau):
+    """Whatever their sum would be, the draw does not fall there."""
+    V = 40000
+    x = torch.full((N, V), low, device="cuda", dtype=DT[dtype])
+    x[:, 3000:3010] = top
+    u = np.float32([0.0, 1.0, 0.55] * (N // 3))
+    tok, q = check_draw(x, np.full(N, tau, np.float32), u)
+    assert tok[:3].tolist() == [3000, 3009, 3005] and (q == np.float32(0.1)).all()
+
+
 def test_draw_every_kind_of_not_a_number():
     """Quiet and signalling ones of either sign, as bf16 bit patterns."""
     V = 5000
