@@ -152,3 +152,23 @@ def test_resident_loop_with_masks_and_a_small_pool():
             break
     assert res.lengths.tolist() == [L] * B and waited > 0
     assert res.report()["finished"] == B
+
+
+@pytest.mark.gpu
+@pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")
+@pytest.mark.parametrize("tau", [0.0, 0.8])
+def test_resident_step_does_not_wait_for_the_gpu(tau):
+    """Behind work that takes the GPU tens of milliseconds, a step (about one) returns
+    while that still runs."""
+    m = drv.TableModels(500, R=16, seed=2, device=torch.device("cuda"))
+    res = drv.ResidentDecoder(m, 4, 2, tau, seed=3, max_tokens=200, presence=0.5)
+    for _ in range(8):
+        res.step()
+    torch.cuda.synchronize()
+    behind = torch.cuda.Event()
+    torch.cuda._sleep(50_000_000)       # cycles of a clock between 100 MHz and 2.4 GHz
+    behind.record()
+    res.step()
+    running = not behind.query()
+    torch.cuda.synchronize()
+    assert running
