@@ -209,7 +209,8 @@ class ResidentDecoder:
     repetition, frequency, presence: penalties, a number or one per request;
     bias_ids, bias_values [B, n], mask [M, ceil(V / 32)] with mask_index [B, K+1]: as
     ``shape_logits`` takes them, applied to all three views; pool: blocks of the
-    store (default: enough for every request)."""
+    store (default: enough for every request); device: that of the models (the
+    default), on which all of it runs."""
 
     def __init__(self, models: TableModels, B: int, K: int, temperature, beta: float = 1.0,
                  gamma: float = 0.5, gate_mode: int = 0, seed: int = 0, device=None, early_exit: int = 0,
@@ -222,6 +223,9 @@ class ResidentDecoder:
             raise ValueError("the decoder needs TableModels(device=...)")
         self._torch, self._asp = torch, asp
         self.m, self.B, self.K, self.device = models, B, K, models.dev[0].device
+        want = self.device if device is None else torch.device(device)
+        if want.type != self.device.type or want.index not in (None, self.device.index):
+            raise ValueError(f"the models are on device {self.device}, not on {want}")
         self.rng = np.random.default_rng(seed)
         self.kw = dict(beta=beta, gamma=gamma, gate_mode=gate_mode, early_exit=early_exit, fuse_bonus=fuse_bonus,
                        workspace=asp.Workspace(self.device))

@@ -172,3 +172,11 @@ def test_resident_step_does_not_wait_for_the_gpu(tau):
     running = not behind.query()
     torch.cuda.synchronize()
     assert running
+
+
+def test_resident_loop_runs_on_its_models_device():
+    """`device` may name it; another one is refused, not ignored."""
+    m = drv.TableModels(50, R=8, device="cpu")
+    for other in ("cuda", "cuda:1", torch.device("cuda", 0)):
+        with pytest.raises(ValueError, match="device"):
+            drv.ResidentDecoder(m, 2, 1, 0.0, device=other)
