@@ -24,7 +24,7 @@ constexpr uint32_t kNegInfBits = 0xFF800000u;
 template <int DT> struct Row;
 
 template <> struct Row<ASYMSPEC_BF16> {
-  static constexpr int VE = 8, kBytes = 2;
+  static constexpr int VE = 8;
   typedef uint16_t T;
   typedef uint32_t U __attribute__((ext_vector_type(4), aligned(2)));
   static STEP_DEV float get(const u4& v, int e) {
@@ -50,13 +50,12 @@ template <> struct Row<ASYMSPEC_BF16> {
       v[i] = (v[i] & keep) | (0xFF80FF80u & ~keep);
     }
   }
-  static STEP_DEV T elem(const u4& v, int e) { return (T)(v[e >> 1] >> (16 * (e & 1))); }
   static STEP_DEV float get1(T b) { return __uint_as_float((uint32_t)b << 16); }
   static STEP_DEV T put1(float f) { return (T)bits(f); }
 };
 
 template <> struct Row<ASYMSPEC_FP32> {
-  static constexpr int VE = 4, kBytes = 4;
+  static constexpr int VE = 4;
   typedef uint32_t T;
   typedef uint32_t U __attribute__((ext_vector_type(4), aligned(4)));
   static STEP_DEV float get(const u4& v, int e) { return __uint_as_float(v[e]); }
@@ -67,7 +66,6 @@ template <> struct Row<ASYMSPEC_FP32> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = ((allowed >> i) & 1u) ? v[i] : kNegInfBits;
   }
-  static STEP_DEV T elem(const u4& v, int e) { return v[e]; }
   static STEP_DEV float get1(T b) { return __uint_as_float(b); }
   static STEP_DEV T put1(float f) { return __float_as_uint(f); }
 };
