@@ -9,21 +9,19 @@
 
 namespace asym_step {
 
+// Spans without a byte overlap none.
 struct Span {
-  const void* p;
-  size_t bytes;       // 0: no array
+  uintptr_t from, to;
+  Span(const void* p, size_t bytes) : from(bytes != 0 ? (uintptr_t)p : 0), to(from + bytes) {}
 };
 
-// Whether one of the first `written` spans shares a byte with any other one.
+// Whether one of the first `written` spans shares a byte with any other one.  (No branch
+// in the loop: a call that is bound by what the host does compares some 50 pairs.)
 inline bool overlap(const Span* s, int written, int n) {
-  for (int i = 0; i < written; ++i) {
-    const uintptr_t a0 = (uintptr_t)s[i].p, a1 = a0 + s[i].bytes;
-    for (int j = i + 1; j < n; ++j) {
-      const uintptr_t b0 = (uintptr_t)s[j].p, b1 = b0 + s[j].bytes;
-      if (a0 < b1 && b0 < a1 && s[i].bytes != 0 && s[j].bytes != 0) return true;
-    }
-  }
-  return false;
+  bool any = false;
+  for (int i = 0; i < written; ++i)
+    for (int j = i + 1; j < n; ++j) any |= (s[i].from < s[j].to) & (s[j].from < s[i].to);
+  return any;
 }
 
 // The same for plan_slots, whose workgroups read all requests while others already
@@ -33,7 +31,7 @@ inline bool slots_overlap(const void* lengths, const void* new_tokens, const voi
                           int width, int total, const void* slots, const void* starts, const void* short_out,
                           const void* n_blocks_out, const void* state_out) {
   const size_t b = (size_t)B * 4;
-  auto of = [](const void* p, size_t bytes) { return Span{p, p != nullptr ? bytes : 0}; };
+  auto of = [](const void* p, size_t bytes) { return Span(p, p != nullptr ? bytes : 0); };
   const Span s[] = {of(table, b * (size_t)max_blocks), of(ring, (size_t)ring_size * 4),
                     of(slots, (width > 0 ? (size_t)B * (size_t)width : (size_t)total) * 8), of(starts, b + 4),
                     of(short_out, b), of(n_blocks_out, b), of(state_out, 8),
