@@ -460,9 +460,10 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
   asym::wave_scan_d(mine, upto, ahead);
   const double total = __shfl(upto, 63, 64);
   const double target = (double)u * total;
-  // the first lane whose sums pass the target; without one (a uniform of 1) the
-  // last lane with weight
-  const unsigned long long past = __ballot(upto > target && mine > 0.0), some = __ballot(mine > 0.0);
+  // the first lane whose sums pass the target; without one, and with a uniform of 1 (which
+  // a lane's sums can pass, too: they may be rounded to more than the total), the last
+  // lane with weight
+  const unsigned long long past = __ballot(u < 1.0f && upto > target && mine > 0.0), some = __ballot(mine > 0.0);
   const bool none = past == 0ull;
   const int from = none ? 63 - __clzll((long long)(some | 1ull)) : __ffsll(past) - 1;
   int at = lo;

@@ -360,6 +360,19 @@ def test_draw_of_a_chunk_whose_tokens_have_no_weight(dtype, N, low, top, tau):
     assert tok[:3].tolist() == [3000, 3009, 3005] and (q == np.float32(0.1)).all()
 
 
+@pytest.mark.parametrize("N,V,dtype", [(700, 30000, "bf16"), (200, 70001, "bf16"), (300, 9000, "fp32"), (64, 300000, "fp32")])
+def test_draw_with_uniforms_of_one_and_more(N, V, dtype):
+    """The last token with weight, also where sums over fewer tokens are rounded to
+    more than the row's."""
+    x, _ = stored(np.random.default_rng(N), (N, V), dtype)
+    x[:, V - 4000:] -= 45.0                  # so little weight that it adds nothing to a sum
+    x[::2, V - 1 - N:] = -math.inf
+    u = np.resize(np.float32([1.0, 1.0, 1.5, math.inf]), N)
+    tok, _ = asp.draw_tokens(x, torch.full((N,), 1.0, device="cuda"), gpu(u))
+    want = np.where(np.arange(N) % 2 == 0, V - 2 - N, V - 1)
+    assert np.array_equal(tok.cpu().numpy(), want)
+
+
 def test_draw_every_kind_of_not_a_number():
     """Quiet and signalling ones of either sign, as bf16 bit patterns."""
     V = 5000
