@@ -141,10 +141,8 @@ void* stream_of(PyObject* o) {
 }
 
 // The outputs of a call: the caller's tensors, or new ones, which share one
-// allocation (each costs about as much as the launch's own share), but for those of more
-// than 64 KB: a tensor that a program keeps would keep them.
+// allocation (each costs about as much as the launch's own share).
 struct Outs {
-  static constexpr size_t kOwn = 64u << 10;
   PyObject* tuple;
   Tensor own[5];
   const Tensor* at[5] = {};
@@ -152,9 +150,8 @@ struct Outs {
   at::ScalarType type[5];
   int64_t shape[5][2];
   int dims[5];
-  bool apart[5] = {};
   int n, said = 0;
-  size_t bytes = 0;                 // of those that share
+  size_t bytes = 0;
   Outs(PyObject* o, int n_) : tuple(o), n(n_) {
     if (o == Py_None) return;
     if (!PyTuple_Check(o) && !PyList_Check(o)) refuse("out must be a tuple of tensors", PyExc_TypeError);
@@ -175,26 +172,23 @@ struct Outs {
     dims[i] = d1 < 0 ? 1 : 2;
     offset[i] = bytes;
     const size_t size = (size_t)d0 * (d1 < 0 ? 1 : (size_t)d1) * c10::elementSize(t);
-    if (size <= kOwn) bytes += (size + 15) / 16 * 16;
-    else apart[i] = true;
+    bytes += (size + 15) / 16 * 16;
   }
   // Makes the new ones, and `extra` bytes behind them, whose address it returns.
   void* make(const at::Device& dev, size_t extra = 0) {
-    const size_t mine = made() ? bytes : 0, all = mine + extra;
-    if (all != 0) base = at::empty({(int64_t)all}, at::TensorOptions().dtype(at::kByte).device(dev));
-    for (int i = 0; made() && i < n; ++i) {
-      at[i] = &own[i];
-      if (apart[i]) {
-        own[i] = at::empty(sizes(i), at::TensorOptions().dtype(type[i]).device(dev));
-        continue;
-      }
+    const size_t all = (made() ? bytes : 0) + extra;
+    if (all == 0) return nullptr;
+    base = at::empty({(int64_t)all}, at::TensorOptions().dtype(at::kByte).device(dev));
+    if (!made()) return base.data_ptr();
+    for (int i = 0; i < n; ++i) {
       auto t = c10::make_intrusive<c10::TensorImpl>(c10::Storage(base.storage()), base.key_set(),
                                                     c10::scalarTypeToTypeMeta(type[i]));
       t->set_storage_offset((int64_t)(offset[i] / c10::elementSize(type[i])));
       t->set_sizes_contiguous(sizes(i));
       own[i] = Tensor(std::move(t));
+      at[i] = &own[i];
     }
-    return all != 0 ? (char*)base.data_ptr() + mine : nullptr;
+    return (char*)base.data_ptr() + bytes;
   }
   // Address of output i, which has to be as said.
   template <class T>

@@ -6,6 +6,8 @@
 on that device; index tensors are int32.  The calls may be captured into a HIP
 graph.  No gradient passes through them: a tensor that a call writes to must not
 require one (under torch.no_grad() it may), and has a new version afterwards.
+The new outputs of a call share one allocation, which the last of them that is
+kept frees (clone() one that is to be kept without the others, or give `out`).
 There is no fallback: if a library is missing, every call raises.
 """
 

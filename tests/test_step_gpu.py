@@ -720,14 +720,3 @@ def test_slots_overlaps_are_refused_by_the_c_entry():
         assert call(**over) == asp.E_ARG, over
     torch.cuda.synchronize()
     assert torch.equal(room, keep)
-
-
-def test_slots_outputs_keep_no_large_memory():
-    """The requests' state that a program keeps does not keep the slots of a step."""
-    B, n = 64, 200000
-    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")     # noqa: E731
-    for kw in (dict(total=n), dict(width=n // B)):
-        _, *kept = asp.plan_slots(i(B), i(B), i(B, 4), i(B), i(8), i(2), 16, **kw)
-        assert all(t.untyped_storage().nbytes() <= 1 << 16 for t in kept)
-    *kept, tokens, counts = asp.commit_tokens(i(4000), i(4000), i(4000, 8), i(4000, 10), i(4000))
-    assert all(t.untyped_storage().nbytes() <= 1 << 16 for t in (*kept, counts))
