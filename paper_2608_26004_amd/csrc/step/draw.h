@@ -102,17 +102,18 @@ struct DrawScale {
     for (int i = 7; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
     return __builtin_ldexp(p, (int)(uint32_t)__builtin_bit_cast(uint64_t, s));
   }
-  // what a chunk's sum is to be multiplied with
+  // A chunk's sum at the row's level m.  (Scaled at the end: the step between the two
+  // levels alone may be beyond fp64's range.)
   STEP_DEV double of_part(const DrawPart& q) const {
-    if ((q.arg != kPlain && q.arg != kTabled) || inf) return weight((double)(inf ? flat(q.m) : q.m));
-    // 2^(rint(k q.m) - k m), or 2^(-k m)
+    if ((q.arg != kPlain && q.arg != kTabled) || inf) return q.sum * weight((double)(inf ? flat(q.m) : q.m));
+    // times 2^(rint(k q.m) - k m), or 2^(-k m)
     const double at = q.arg == kPlain ? __builtin_rint(k * (double)q.m) : 0.0;
     const double d = __builtin_fmax(__builtin_fma(-k, m, at), -2200.0);
     const double n = __builtin_rint(d), f = d - n;
     double p = __builtin_fma(c[9], f, c[8]);
 #pragma unroll
     for (int i = 7; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
-    return __builtin_ldexp(p, (int)n);
+    return __builtin_ldexp(q.sum * p, (int)n);
   }
 };
 
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(64) void draw_pick_kernel(DrawArgs A) {
   // or more: below that a chunk's sum can come out as more than nothing where none of its
   // tokens has any weight.
   const float least_m = k.inf ? inf : (float)(k.m + k.least * (744.4400719213812 / 762.0));
-  auto weight_of = [&](const DrawPart& q) { return q.m >= least_m ? q.sum * k.of_part(q) : 0.0; };
+  auto weight_of = [&](const DrawPart& q) { return q.m >= least_m ? k.of_part(q) : 0.0; };
   double mine = 0.0, upto, ahead;
   each([&](int, DrawPart& q) {
     const double w = weight_of(q);

@@ -373,6 +373,18 @@ def test_draw_with_uniforms_of_one_and_more(N, V, dtype):
     assert np.array_equal(tok.cpu().numpy(), want)
 
 
+def test_draw_of_chunks_far_below_the_largest():
+    """Weights of 2^-862 in chunks that a table sums at the level 2^833, beside a
+    largest logit beyond the table: counted, though 2^-1695, what is between the two
+    levels, is below fp64's range."""
+    N, V = 300, 40000
+    x = torch.full((N, V), -math.inf, dtype=torch.bfloat16, device="cuda")
+    x[:, 3000:3010], x[:, 20000], x[:, 39000:39005] = 57.75, 117.5, 57.75
+    u = np.resize(np.float32([0.0, 1.0, 0.5]), N)
+    tok, _ = check_draw(x, np.full(N, 0.1, np.float32), u)
+    assert tok[:3].tolist() == [3000, 39004, 20000]
+
+
 def test_draw_every_kind_of_not_a_number():
     """Quiet and signalling ones of either sign, as bf16 bit patterns."""
     V = 5000
