@@ -21,8 +21,9 @@
 // a read's time.  Chunks of 2048 tokens take 4% less on the large batch, but 0.7 us more
 // on one row and in draw_pick; two chunks a wave, or waves that stay and fetch their next
 // chunk ahead, take 4 to 6% more (a SIMD then holds seven waves in place of eight).
-// draw_table takes 55 to 60 us there, near a read's time; for 128 rows of 151936 tokens 13 us
-// against 16, 1 to 2 of them the table's making.  draw_pick takes 4 to 5 us.
+// draw_table takes 55 to 61 us there, near a read's time; for 128 rows of 151936 tokens 13 us
+// against 16, 1 to 2 of them the table's making.  draw_pick takes 4 to 5 us.  fp32 rows, all
+// in draw_part: 65 us for 256 of 256000 (the same bytes), 47 greedy (partly from the cache).
 
 #ifndef ASYMSPEC_STEP_DRAW_H_
 #define ASYMSPEC_STEP_DRAW_H_
@@ -268,14 +269,17 @@ __global__ __launch_bounds__(kDrawThreads) void draw_part_kernel(DrawArgs A) {
 
 // The same for bf16 rows of many chunks: a logit has 16 bits, so a workgroup computes the
 // weights 2^(k l) of all logits with 2^-12 <= |l| < 128 once, into a table of 4864 entries in
-// LDS, and looks its chunks' tokens up: 6 operations a token in place of 17, two tokens at a
-// time where they have 16 bits, and no maximum, as 2^(k l) itself is in fp64's range.  Masked
-// tokens have an entry without weight, smaller logits and zeros (one chunk in 16 has
+// LDS, and looks its chunks' tokens up: 7 operations a token in place of 17, two tokens at a
+// time where they have 16 bits.  2^(k l) itself is in fp64's range, so the sum does not wait
+// for the chunk's largest logit; that is found beside it (a token's half operation, and 8
+// a chunk; 1% of the time of 512 rows of 256000) for the row's level, to which draw_pick
+// brings the sums: at 2^(k l) those of a long row could pass fp64's range, and what has
+// weight would depend on where the logits lie.  Masked tokens have an entry without weight, smaller logits and zeros (one chunk in 16 has
 // one, at a deviation of 3) are computed where they stand.  A chunk with other logits, or
 // with |k l| >= 1000, goes the other way afterwards, as do those behind two such at a wave's
 // start, rows whose temperature makes that likely, and greedy rows.  That order costs rows
-// of such logits throughout: 512 x 256000 of deviation 300 take 111 us (163 if every chunk
-// were tried first; 98 in draw_part), 128 x 151936 30 (20).
+// of such logits throughout: 512 x 256000 of deviation 300 take 114 us (98 in draw_part; 163
+// in the table's kernel if every chunk were tried first), 128 x 151936 32 (20).
 constexpr int kTableThreads = 1024;       // (with 512 and two tables more a unit 18.1 us for 128 rows, 17.0 so)
 constexpr int kTableMost = 64 * (kTableThreads / 64);             // chunks of a workgroup: one bit each a wave
 constexpr uint32_t kTableLow = 0x3980u, kTableHigh = 0x4300u;     // bits of 2^-12 and 128

@@ -26,8 +26,9 @@
 // for each 16-byte vector is 0.4 us.  So what concerns a row is the wave's and stays
 // in scalar registers, and the formula (some 300 operations a vector) runs over the
 // list with no lane idle.  Measured there, behind 8192 tokens: 113 to 115 us with masks (a
-// quarter of them nearly empty, the others 2% of the tokens; the lines touched would
-// take 81), about 75 of them the masks', 20 the lists', 8 the formula's.  Where it took 123,
+// quarter of them nearly empty, the others 2% of the tokens; at those rates the lines touched
+// would take 81, and a kernel that knows them beforehand and does nothing else takes 89 to
+// 93), about 75 of them the masks', 20 the lists', 8 the formula's.  Where it took 123,
 // reading and blending vectors that are masked in part, where now 2-byte stores of -inf
 // go: 137; all masks ahead of the lists: 133 (lines with both changes are then touched
 // twice); listing tokens in place of vectors, a lane each: 156.

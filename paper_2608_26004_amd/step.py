@@ -87,8 +87,11 @@ def draw_tokens(logits, temperature, uniforms, out=None):
     (<= 0: the lowest index of the largest logit, q = 1); uniforms: [N] float32 in
     [0, 1), for an inverse-CDF draw from softmax(logits / temperature), summed in
     fp64; out: (token, q) tensors to write, views such as draft_tokens[:, i]
-    among them.  Logits of -inf or not a number have no weight; a row without any
-    gives token 0 with q = 0.  The workspace is memory of the call's own, from
+    among them, which must overlap no other tensor of the call.  Logits of -inf or
+    not a number have no weight, as those whose weight beside the row's largest is
+    below fp64's smallest number; uniforms of 1 and more give the last token with
+    weight, those below 0 or not a number count as 0; a row without any weight gives
+    token 0 with q = 0.  The workspace is memory of the call's own, from
     torch's allocator: a Workspace holds what fuse_verify knows again, and a
     captured call must not work in memory that a later one replaces."""
     return (_step or _bind()).draw_tokens(logits, temperature, uniforms, out, _stream(logits))
@@ -105,7 +108,8 @@ def commit_tokens(accept_len, next_token, draft_tokens, history, lengths, finish
     ends with the first of them); max_lengths: [B] or None (L).
     Returns (lengths [B], finished [B], tokens [B, K+1] committed, then -1,
     counts [B]), all int32 and new unless given as `out`; out's lengths and
-    finished may be the inputs."""
+    finished may be the inputs, and otherwise what is written (history among it) must
+    overlap no other tensor of the call."""
     return (_step or _bind()).commit_tokens(accept_len, next_token, draft_tokens, history, lengths, finished,
                                             stop_tokens, max_lengths, out, _stream(history))
 
