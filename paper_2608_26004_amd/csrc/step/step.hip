@@ -157,11 +157,11 @@ int asymspec_shape_logits(const asymspec_shape* shape, void* stream) {
   // A workgroup's lists cost the same however few tokens it has, and some copy or mask
   // while others list.  So parts grow until a workgroup has enough to do: 20 KB of rows to
   // copy, 40 KB under masks, and what there is where only listed vectors change; but not
-  // to two workgroups a unit or fewer.  Copies: 96 x 6 rows of 50257 fp32 tokens 58 us
-  // with 24 KB, 63 with 48; 128 x 1 of 151936 bf16 24 with 16 KB, 36 with 8; 16 x 3 of 256000
+  // to two workgroups a unit or fewer.  Copies: 96 x 6 rows of 50257 fp32 tokens 60 us
+  // with 24 KB, 65 with 48; 128 x 1 of 151936 bf16 24 with 16 KB, 36 with 8; 16 x 3 of 256000
   // behind 16000 20 with 24 KB (1008 workgroups), 26 with 12 or with 48 (512).  Masks:
-  // 128 x 7 rows of 151936 121 us with 56 KB, 132 with 28 or 112.  Neither: 8 x 3 behind 4096
-  // 8.9 us with 600 workgroups, 10.1 with 304 or 1192.
+  // 128 x 7 rows of 151936 115 us with 56 KB, 131 with 28, 122 with 112.  Neither: 8 x 3 behind
+  // 4096 8.9 us with 600 workgroups, 10.0 with 304, 9.6 with 1192.
   const int64_t want = s.logits != s.out ? 20 << 10 : s.mask != nullptr ? 40 << 10 : INT64_MAX;
   int T = kShapeMinTokens;
   while (T < kShapeMaxTokens && ((s.R * T * (int64_t)el < want && workgroups(2 * T) > 2ll * cus) ||
