@@ -199,10 +199,9 @@ int asymspec_commit_tokens(const int32_t* accept_len, const int32_t* next_token,
  *   short_out      [B] out: 1 where the request is short, else 0
  *   n_blocks_out   [B] out; free_state_out [2] out.  Neither is its input
  * What the call writes (block_table and free_ring among it) overlaps no other of
- * its arrays; a call of which something does is refused.  1 <= B <= 4096, block_size >= 1,
- * max_blocks >= 1, ring_size >= 1, B * max_blocks, B * width and
- * ring_size below 2^31; with width = 0,
- * total >= 1 and new_tokens is given.
+ * its arrays (checked: ASYMSPEC_E_ARG).  1 <= B <= 4096, block_size >= 1,
+ * max_blocks >= 1, ring_size >= 1, B * max_blocks, B * width and ring_size below
+ * 2^31; with width = 0, total >= 1 and new_tokens is given.
  */
 int asymspec_plan_slots(const int32_t* lengths, const int32_t* new_tokens, const int32_t* release,
                         int32_t* block_table, int max_blocks, const int32_t* n_blocks,

@@ -274,11 +274,11 @@ __global__ __launch_bounds__(kDrawThreads) void draw_part_kernel(DrawArgs A) {
 // for the chunk's largest logit; that is found beside it (a token's half operation, and 8
 // a chunk; 1% of the time of 512 rows of 256000) for the row's level, to which draw_pick
 // brings the sums: at 2^(k l) those of a long row could pass fp64's range, and what has
-// weight would depend on where the logits lie.  Masked tokens have an entry without weight, smaller logits and zeros (one chunk in 16 has
-// one, at a deviation of 3) are computed where they stand.  A chunk with other logits, or
-// with |k l| >= 1000, goes the other way afterwards, as do those behind two such at a wave's
-// start, rows whose temperature makes that likely, and greedy rows.  That order costs rows
-// of such logits throughout: 512 x 256000 of deviation 300 take 114 us (98 in draw_part; 163
+// weight would depend on where the logits lie.  Masked tokens have an entry without weight,
+// smaller logits and zeros (one chunk in 16 has one, at a deviation of 3) are computed where
+// they stand.  A chunk with other logits, or with |k l| >= 1000, goes the other way
+// afterwards, as do those behind two such at a wave's start, rows whose temperature makes
+// that likely, and greedy rows.  That order costs rows of such logits throughout: 512 x 256000 of deviation 300 take 114 us (98 in draw_part; 163
 // in the table's kernel if every chunk were tried first), 128 x 151936 32 (20).
 constexpr int kTableThreads = 1024;       // (with 512 and two tables more a unit 18.1 us for 128 rows, 17.0 so)
 constexpr int kTableMost = 64 * (kTableThreads / 64);             // chunks of a workgroup: one bit each a wave
