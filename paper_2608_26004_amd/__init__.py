@@ -12,6 +12,7 @@ import ctypes
 import os
 
 __all__ = ["fuse_verify", "shape_logits", "draw_tokens", "commit_tokens", "plan_slots",
+           "new_cache", "rotary_frequencies", "rotate_heads", "write_cache", "read_cache", "attend_cache",
            "workspace_size", "Workspace", "load_library", "status_string",
            "workspace_timeouts", "set_wait_limit",
            "BF16", "FP32", "GATE_CDA", "GATE_FIXED", "GATE_KL", "GATE_LAMBDA",
@@ -258,14 +259,17 @@ def fuse_verify(t, a, b, draft_tokens, draft_probs, uniforms, temperature,
     return res
 
 
-# the operators around the decision step (step.py), loaded at their first use
+# the operators around the decision step (step.py) and of the cache (cache.py), loaded at
+# their first use
 _STEP = ("shape_logits", "draw_tokens", "commit_tokens", "plan_slots")
+_CACHE = ("new_cache", "rotary_frequencies", "rotate_heads", "write_cache", "read_cache", "attend_cache")
 
 
 def __getattr__(name):
-    if name in _STEP:
-        from . import step
-        for n in _STEP:
-            globals()[n] = getattr(step, n)
+    if name in _STEP or name in _CACHE:
+        from . import cache, step
+        for names, module in ((_STEP, step), (_CACHE, cache)):
+            for n in names:
+                globals()[n] = getattr(module, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

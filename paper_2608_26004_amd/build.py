@@ -27,10 +27,18 @@ FLAGS = [
 
 def units():
     """(object name, source, defines) of every object of the library: the host
-    side, the operators around the decision step, the cross-family kernels per
-    storage type, and one object per instance of the decision kernel (storage
-    type x source of delta x variant), compiled in parallel."""
-    out = [("asymspec", "asymspec.hip", []), ("step", os.path.join("step", "step.hip"), [])]
+    side, the operators around the decision step and those of the cache, the
+    attention's kernels per width of codes, type of queries and kind of block size,
+    the cross-family kernels per storage type, and one object per instance of the
+    decision kernel (storage type x source of delta x variant), compiled in parallel."""
+    out = [("asymspec", "asymspec.hip", []), ("step", os.path.join("step", "step.hip"), []),
+           ("cache", os.path.join("cache", "cache.hip"), [])]
+    for bits in (4, 8):
+        for dt in (1, 0):
+            for whole in (0, 1):
+                out.insert(0, (f"attend_{bits}{dt}{whole}", os.path.join("cache", "attend.hip"),
+                               [f"-DASYMSPEC_PART_BITS={bits}", f"-DASYMSPEC_PART_DT={dt}",
+                                f"-DASYMSPEC_PART_WHOLE={whole}"]))
     for dt in (0, 1):
         out.append((f"xv_{dt}", "xvocab.hip", [f"-DASYMSPEC_PART_DT={dt}"]))
         for dm in (0, 1, 2):
@@ -108,13 +116,13 @@ def build_example(verbose: bool = False) -> str:
     return EXAMPLE
 
 
-BIND_SRC = os.path.join(CSRC, "step", "bind.cpp")
+BIND_SRC = [os.path.join(CSRC, "step", "bind.cpp"), os.path.join(CSRC, "cache", "bind.cpp")]
 BIND = os.path.join(HERE, "_step.so")
 
 
 def build_binding(verbose: bool = False) -> str:
-    """_step.so: the Python binding of the operators around the decision step,
-    host code against torch's C++ interface, linked to libasymspec.so."""
+    """_step.so: the Python binding of the operators around the decision step and of
+    the cache, host code against torch's C++ interface, linked to libasymspec.so."""
     import sysconfig
 
     import torch
@@ -124,7 +132,7 @@ def build_binding(verbose: bool = False) -> str:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-isystem", os.path.join(at, "include"),
            "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include", "-I", INC, BIND_SRC,
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include", "-I", INC, *BIND_SRC,
            "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
            "-L", HERE, "-lasymspec", "-L", "/opt/rocm/lib", "-lamdhip64", "-Wl,-rpath,$ORIGIN", "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -1,0 +1,614 @@
+// attend_cache: softmax(scale q k^T) v over a paged cache in 8 or 4 bits, in one pass.
+//
+// Work is cut along the cache: a unit is 128 positions of one head of the cache, for
+// all rows of the step and all query heads that read it (16 MT of these rows at a
+// time).  The units of all requests form one list, which the workgroups share evenly,
+// whatever the requests' lengths: each takes a run of neighbouring units, of which
+// each of its four waves takes 32 positions.  A wave keeps a running reference and sum
+// for each row, so that nothing is exchanged until a run ends; there the waves' parts
+// meet in LDS, and parts of different workgroups in memory, which a second kernel
+// joins.
+//
+// Both products run on 16x16x32 bf16 matrix instructions.  For the scores a lane
+// decodes what it loaded, with the order of the channels permuted alike on both sides
+// so that a lane's piece of a key is contiguous; the scores come out as the second
+// product's operand needs its probabilities (one row a lane, four positions in a row),
+// so that those never move between lanes.  A lane loads the same channels of eight
+// positions of the values and pairs them by byte permutes.
+
+#ifndef ASYMSPEC_CACHE_ATTEND_H_
+#define ASYMSPEC_CACHE_ATTEND_H_
+
+#include "format.h"
+
+namespace asym_cache {
+
+constexpr int kAttendThreads = 256;
+constexpr int kUnit = 128;                        // positions of a unit: 32 a wave
+constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+struct AttendArgs {
+  asymspec_attend a;
+  float* sums;          // [2 workgroups][16 MT][dim]: unfinished runs
+  float2* stats;        // [2 workgroups][16 MT]: reference, sum
+  int* starts;          // [B + 1]: the requests' first units
+  int group;            // query heads of a head of the cache
+  int rows;             // R * group
+  int row_tiles;        // of 16 MT rows
+  int most;             // positions that a table holds
+  int workgroups;
+  float c;              // scale * log2 e
+  Div by_size, by_group;
+};
+
+// A head's channels in pieces of 128, 64 or 32, of which a lane holds a quarter of a
+// key's (contiguous), or a sixteenth of a value's.
+template <int D> struct Pieces {
+  static constexpr int N = (D == 64 || D == 128) ? 1 : 2;
+  static constexpr int width(int i) { return D == 96 ? (i == 0 ? 64 : 32) : D == 192 ? (i == 0 ? 128 : 64) : D == 64 ? 64 : 128; }
+  static constexpr int base(int i) { return i == 0 ? 0 : width(0); }
+};
+
+// What a request has for its rows: units from `first` on that hold its positions
+// [lo, hi), and its number of rows.
+struct Range {
+  int len, fresh, lo, hi, first, units;
+  STEP_DEV Range(const AttendArgs& A, int b) {
+    len = min(max(A.a.lengths[b], 0), 0x7FFFFF00);
+    fresh = A.a.new_tokens != nullptr ? min(max(A.a.new_tokens[b], 0), A.a.R) : A.a.R;
+    hi = min(len + fresh, A.most);
+    lo = A.a.window > 0 ? max(0, len - A.a.window + 1) : 0;
+    first = lo / kUnit;
+    units = fresh > 0 && hi > lo ? (hi + kUnit - 1) / kUnit - first : 0;
+  }
+};
+
+STEP_DEV float lanes_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+STEP_DEV float lanes_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+STEP_DEV uint32_t bf_pair(float a, float b) {
+  const bf2 r = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, r);
+}
+STEP_DEV float bf_low(uint32_t x) { return __uint_as_float(x << 16); }
+STEP_DEV float bf_high(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+
+STEP_DEV f4 mfma(const u4& a, const u4& b, const f4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+// 8 fp32 values as N bf16 parts that add up to them, but for 2^-8N of each.
+template <int N>
+STEP_DEV void split8(const float* x, u4* parts) {
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+#pragma unroll
+  for (int p = 0; p < N; ++p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      parts[p][i] = bf_pair(rest[2 * i], rest[2 * i + 1]);
+      if (p + 1 < N) {
+        rest[2 * i] -= bf_low(parts[p][i]);
+        rest[2 * i + 1] -= bf_high(parts[p][i]);
+      }
+    }
+  }
+}
+
+// A one in each byte that is an e4m3 code of no number.
+STEP_DEV uint32_t nan_codes(uint32_t x) { return (((x & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u; }
+
+template <int BYTES>
+STEP_DEV void load_codes(const uint8_t* p, uint32_t* r) {
+  if constexpr (BYTES == 1) r[0] = *p;
+  else if constexpr (BYTES == 2) r[0] = *(const uint16_t*)p;
+  else if constexpr (BYTES == 4) r[0] = *(const uint32_t*)p;
+  else if constexpr (BYTES == 8) {
+    const u2 v = *(const u2*)p;
+    r[0] = v[0], r[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < BYTES / 16; ++i) {
+      const u4 v = *(const u4*)(p + 16 * i);
+      r[4 * i] = v[0], r[4 * i + 1] = v[1], r[4 * i + 2] = v[2], r[4 * i + 3] = v[3];
+    }
+  }
+}
+
+// f(integral constant) for 0 .. N - 1
+template <int N, int I = 0, class F>
+STEP_DEV void count(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    count<N, I + 1>(f);
+  }
+}
+
+// 32 positions' codes as a wave's lanes load them: with j = lane % 16 and h = lane / 16,
+// of the keys of positions 16 a + j a quarter of each piece, of the values of
+// positions 4 h + i and 16 + 4 h + i a sixteenth.
+template <int BITS, int D>
+struct Codes {
+  typedef Pieces<D> P;
+  static constexpr int kKey = D * BITS / 128, kVal = BITS / 4 * P::N;     // dwords
+  uint32_t key[2][kKey], val[8][kVal] = {};
+  uint8_t key_scale[2][P::N], val_scale[8][P::N];
+
+  STEP_DEV void load(const asymspec_cache& c, const uint32_t* key_row, const uint32_t* val_row, int j, int h) {
+    constexpr uint32_t kRow = D * BITS / 8, kScales = D / kBlock;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const uint8_t* k = (const uint8_t*)c.keys + (uint64_t)key_row[a] * kRow;
+      const uint8_t* s = (const uint8_t*)c.key_scales + (uint64_t)key_row[a] * kScales;
+      count<P::N>([&](auto p) {
+        constexpr int w = P::width(p), from = P::base(p);
+        load_codes<w * BITS / 32>(k + from * BITS / 8 + h * (w * BITS / 32), &key[a][from * BITS / 128]);
+        key_scale[a][p] = s[(from + h * (w / 4)) / kBlock];
+      });
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const uint8_t* v = (const uint8_t*)c.values + (uint64_t)val_row[t] * kRow;
+      const uint8_t* s = (const uint8_t*)c.value_scales + (uint64_t)val_row[t] * kScales;
+      count<P::N>([&](auto p) {
+        constexpr int w = P::width(p), from = P::base(p);
+        load_codes<w * BITS / 128>(v + from * BITS / 8 + j * (w * BITS / 128), &val[t][p * (BITS / 4)]);
+        val_scale[t][p] = s[(from + j * (w / 16)) / kBlock];
+      });
+    }
+  }
+};
+
+// Four channels of a row from its sums, and its lse.
+template <int DT>
+STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int ch, float ref, float sum, const f4& o) {
+  typedef typename Row<DT>::T T;
+  const int64_t at = ((int64_t)b * A.a.R + r) * A.a.q_heads + q_head;
+  const bool none = sum == 0.f;
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : o[e] / sum;
+  T* out = (T*)A.a.out + at * dim + ch;
+  if constexpr (DT == ASYMSPEC_BF16) *(u2*)out = u2{bf_pair(y[0], y[1]), bf_pair(y[2], y[3])};
+  else *(f4*)out = f4{y[0], y[1], y[2], y[3]};
+  if (ch == 0 && A.a.lse != nullptr) A.a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
+}
+
+template <int BITS, int DT, int D, int MT, bool WHOLE>
+__global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
+  typedef Pieces<D> P;
+  typedef Codes<BITS, D> C;
+  typedef typename Row<DT>::T T;
+  constexpr int kParts = DT == ASYMSPEC_BF16 ? 1 : 3;      // of a query
+  constexpr int kProb = DT == ASYMSPEC_BF16 ? 2 : 3;       // of a probability
+  constexpr int kSteps = D / 32, kTiles = D / 16;          // matrix instructions along a head
+  constexpr int kStride = D + 4;                           // of a row in LDS: 16 rows, all banks
+  __shared__ float buf[4][16][kStride];
+  __shared__ float2 stat[4][16];
+  __shared__ int totals[4], found[2];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int j = lane & 15, h = lane >> 4;
+  const int heads = A.a.cache.heads, per_unit = heads * A.row_tiles;
+
+  // The requests' first units in the list, and the request of this workgroup's first one.
+  const int each = (A.a.B + kAttendThreads - 1) / kAttendThreads;
+  int mine = 0;
+  for (int i = 0; i < each; ++i) {
+    const int b = tid * each + i;
+    if (b < A.a.B) mine += Range(A, b).units * per_unit;
+  }
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int below = __shfl_up(upto, d);
+    if (lane >= d) upto += below;
+  }
+  if (lane == 63) totals[wave] = upto;
+  __syncthreads();
+  int start = upto - mine, all = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) start += totals[w];
+    all += totals[w];
+  }
+  const int G = min(A.workgroups, all), me = blockIdx.x;
+  int u = 0, end = 0;
+  if (me < G) {
+    u = (int)((long long)me * all / G);
+    end = (int)((long long)(me + 1) * all / G);
+  }
+  for (int i = 0; i < each; ++i) {
+    const int b = tid * each + i;
+    if (b >= A.a.B) break;
+    const int n = Range(A, b).units * per_unit;
+    if (me == 0) A.starts[b] = start;
+    if (u >= start && u < start + n) found[0] = b, found[1] = start;
+    start += n;
+    if (me == 0 && b == A.a.B - 1) A.starts[A.a.B] = start;
+  }
+  __syncthreads();
+  if (u >= end) return;
+  int b = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
+
+  while (u < end) {
+    const Range range(A, b);
+    const int n = range.units;
+    if (u >= base + n * per_unit) {
+      base += n * per_unit;
+      ++b;
+      continue;
+    }
+    const int run = (u - base) / n, from = (u - base) - run * n, to = min(n, from + (end - u));
+    const int head = run / A.row_tiles, row0 = (run - head * A.row_tiles) * (16 * MT);
+    u += to - from;
+
+    // the queries of this lane's rows, and the positions that these see
+    u4 q[MT][kParts][kSteps];
+    int see_lo[MT], see_hi[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      uint32_t g = (uint32_t)(row0 + 16 * m + j);
+      const bool is = (int)g < A.rows;
+      const int r = is ? (int)A.by_group.split(g) : 0;
+      if (!is) g = 0;
+      see_hi[m] = range.len + r;
+      see_lo[m] = A.a.window > 0 ? range.len + r - A.a.window + 1 : 0;
+      const T* x = (const T*)A.a.q.at + (b * A.a.q.request + r * A.a.q.row + (head * A.group + (int)g) * A.a.q.head);
+      count<P::N>([&](auto p) {
+        constexpr int w = P::width(p), base_ch = P::base(p);
+#pragma unroll
+        for (int s = 0; s < w / 32; ++s) {
+          const T* y = x + base_ch + h * (w / 4) + 8 * s;
+          if constexpr (DT == ASYMSPEC_BF16) {
+            q[m][0][base_ch / 32 + s] = asym_step::load_vec<DT>(y);
+          } else {
+            float f[8];
+            u4 parts[kParts];
+            load8<DT>(y, f);
+            split8<kParts>(f, parts);
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) q[m][k][base_ch / 32 + s] = parts[k];
+          }
+        }
+      });
+    }
+    // positions that every row sees
+    const int full_hi = range.len, full_lo = A.a.window > 0 ? range.len + range.fresh - A.a.window : 0;
+
+    f4 acc[MT][kTiles];
+    float ref[MT], sum[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      ref[m] = -INFINITY;
+      sum[m] = 0.f;
+#pragma unroll
+      for (int e = 0; e < kTiles; ++e) acc[m][e] = f4{0, 0, 0, 0};
+    }
+
+    // Rows of the cache of 32 positions from p on: each lane looks up one position's,
+    // or, with blocks of whole sixteens, its sixteen's first.
+    auto row_of_lane = [&](int p) -> uint32_t {
+      const int position = p + (WHOLE ? lane & 16 : lane & 31);
+      uint32_t offset = (uint32_t)position;
+      const uint32_t page = A.by_size.split(offset);
+      if (position >= A.most) return kNoRow;
+      const int block = A.a.block_table[(int64_t)b * A.a.max_blocks + page];
+      if ((uint32_t)block >= (uint32_t)A.a.cache.blocks) return kNoRow;
+      return ((uint32_t)block * (uint32_t)heads + (uint32_t)head) * (uint32_t)A.a.cache.block_size + offset;
+    };
+    // (what is not there is read from row 0 and left out)
+    auto load = [&](uint32_t row, C& c, uint32_t& there) {
+      there = (uint32_t)__ballot(row != kNoRow);
+      if (row == kNoRow) row = 0;
+      uint32_t kr[2], vr[8];
+      if (WHOLE) {
+        const uint32_t r0 = __builtin_amdgcn_readlane(row, 0), r1 = __builtin_amdgcn_readlane(row, 16);
+        const uint32_t at[2] = {(there & 1u) ? r0 : 0, (there & 0x10000u) ? r1 : 0};
+        // (row 0 alone is sure to be there)
+        const uint32_t one[2] = {(there & 1u) ? 1u : 0u, (there & 0x10000u) ? 1u : 0u};
+#pragma unroll
+        for (int a = 0; a < 2; ++a) kr[a] = at[a] + one[a] * j;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) vr[t] = at[t / 4] + one[t / 4] * (4 * h + t % 4);
+      } else {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) kr[a] = __shfl(row, 16 * a + j);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) vr[t] = __shfl(row, 16 * (t / 4) + 4 * h + t % 4);
+      }
+      c.load(A.a.cache, kr, vr, j, h);
+    };
+
+    const int p_first = (range.first + from) * kUnit + 32 * wave;
+    const int p_end = min(range.hi, (range.first + to) * kUnit);
+    for (int p = p_first; p < p_end; p += kUnit) {
+      if (p + 32 <= range.lo) continue;
+      const uint32_t row = row_of_lane(p);
+      C c;
+      uint32_t there;
+      load(row, c, there);
+      const bool full = there == 0xFFFFFFFFu && p + 31 <= full_hi && p >= full_lo;
+
+      // scores of positions 16 a + 4 h + i
+      f4 s[MT][2];
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s[m][a] = f4{0, 0, 0, 0};
+        count<P::N>([&](auto pc) {
+          constexpr int w = P::width(pc), base_ch = P::base(pc);
+          const float scale = scale_of(c.key_scale[a][pc]);
+#pragma unroll
+          for (int st = 0; st < w / 32; ++st) {
+            const u4 k = decode8<BITS>(&c.key[a][base_ch * BITS / 128 + st * (BITS / 4)], scale);
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int x = 0; x < kParts; ++x) s[m][a] = mfma(k, q[m][x][base_ch / 32 + st], s[m][a]);
+          }
+        });
+      }
+      uint32_t bad_key = 0, bad_val = 0;
+#pragma unroll
+      for (int x = 0; x < P::N; ++x) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) bad_key |= c.key_scale[a][x] > most_scale<BITS>();
+#pragma unroll
+        for (int t = 0; t < 8; ++t) bad_val |= c.val_scale[t][x] > most_scale<BITS>();
+      }
+      if (BITS == 8 && !full) {
+        // (where all rows see all positions, the products spread a code that is not a
+        // number as they should)
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+          for (int x = 0; x < C::kVal; ++x) bad_val |= nan_codes(c.val[t][x]);
+      }
+      if (__any(bad_key)) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          uint32_t of = 0;
+#pragma unroll
+          for (int x = 0; x < P::N; ++x) {
+            const uint64_t lanes = __ballot(c.key_scale[a][x] > most_scale<BITS>());
+            of |= (uint32_t)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xFFFFu;
+          }
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if ((of >> (4 * h + i)) & 1u) s[m][a][i] = NAN;
+        }
+      }
+
+      // probabilities beside the row's reference, which follows its largest score once
+      // that is 2^8 above it
+      u4 prob[MT][kProb];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        uint32_t seen = 0xFFu;
+        float top = -INFINITY;
+        if (!full) {
+          seen = 0;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const int k = 16 * (t / 4) + 4 * h + t % 4;
+            const bool is = ((there >> (WHOLE ? k & 16 : k)) & 1u) && p + k <= see_hi[m] && p + k >= see_lo[m];
+            seen |= (is ? 1u : 0u) << t;
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const float x = s[m][t / 4][t % 4] * A.c;
+          top = fmaxf(top, full || ((seen >> t) & 1u) ? x : -INFINITY);
+        }
+        if (__any(top > ref[m] + 8.f)) {
+          const float next = fmaxf(ref[m], lanes_max(top));
+          const float f = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[m] - next);
+          ref[m] = next;
+          sum[m] *= f;
+#pragma unroll
+          for (int e = 0; e < kTiles; ++e) acc[m][e] *= f;
+        }
+        const float at = ref[m] == -INFINITY ? 0.f : ref[m];
+        float w[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          w[t] = __builtin_amdgcn_exp2f(fmaf(s[m][t / 4][t % 4], A.c, -at));
+          if (!full) w[t] = ((seen >> t) & 1u) ? w[t] : 0.f;
+          sum[m] += w[t];
+        }
+        split8<kProb>(w, prob[m]);
+      }
+
+      float vs[8][P::N];
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+#pragma unroll
+        for (int x = 0; x < P::N; ++x) vs[t][x] = scale_of(c.val_scale[t][x]);
+      if (__any(bad_val)) {
+        // Where a row sees a value that is not a number, the sum becomes one; where it
+        // does not, the value must not count: a probability of 0 would not hide it.
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+#pragma unroll
+          for (int x = 0; x < P::N; ++x)
+            if (c.val_scale[t][x] > most_scale<BITS>()) vs[t][x] = 0.f;
+        if (BITS == 8) {
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int x = 0; x < C::kVal; ++x) c.val[t][x] &= ~(nan_codes(c.val[t][x]) * 0xFFu);
+        }
+        const uint32_t safe = row == kNoRow ? 0 : row;
+        for (int k = 0; k < 32; ++k) {
+          if (!((there >> (WHOLE ? k & 16 : k)) & 1u)) continue;
+          const uint32_t r = WHOLE ? __shfl(safe, k & 16) + (k & 15) : __shfl(safe, k);
+          const uint8_t* scales = (const uint8_t*)A.a.cache.value_scales + (uint64_t)r * (D / kBlock);
+          const uint8_t* codes = (const uint8_t*)A.a.cache.values + (uint64_t)r * (D * BITS / 8);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            if (p + k > see_hi[m] || p + k < see_lo[m]) continue;
+            count<P::N>([&](auto pc) {
+              constexpr int w = P::width(pc), base_ch = P::base(pc);
+#pragma unroll
+              for (int e = 0; e < w / 16; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int ch = base_ch + (4 * h + i) * (w / 16) + e;
+                  if (scales[ch / kBlock] > most_scale<BITS>() || (BITS == 8 && (codes[ch] & 0x7F) == 0x7F))
+                    acc[m][base_ch / 16 + e][i] = NAN;
+                }
+            });
+          }
+        }
+      }
+      count<P::N>([&](auto pc) {
+        constexpr int w = P::width(pc), base_ch = P::base(pc);
+        count<w / 32>([&](auto e2) {
+          constexpr int kSel = BITS == 4 ? e2 : e2 % 2, kReg = pc * (BITS / 4) + (BITS == 4 ? 0 : e2 / 2);
+          uint32_t x[8];
+#pragma unroll
+          for (int t = 0; t < 8; ++t) x[t] = decode2<BITS, kSel>(c.val[t][kReg], vs[t][pc]);
+          u4 even, odd;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            even[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x05040100u);
+            odd[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
+          }
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int k = 0; k < kProb; ++k) {
+              acc[m][base_ch / 16 + 2 * e2] = mfma(even, prob[m][k], acc[m][base_ch / 16 + 2 * e2]);
+              acc[m][base_ch / 16 + 2 * e2 + 1] = mfma(odd, prob[m][k], acc[m][base_ch / 16 + 2 * e2 + 1]);
+            }
+        });
+      });
+    }
+
+    // The four waves' parts of the run, and what becomes of them.
+    const bool complete = from == 0 && to == n;
+    const int slot = 2 * me + (from > 0 ? 0 : 1);       // (a run that an earlier workgroup began comes first)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const float mine_sum = lanes_sum(sum[m]);
+      __syncthreads();
+      if (h == 0) stat[wave][j] = make_float2(ref[m], mine_sum);
+      count<P::N>([&](auto pc) {
+        constexpr int w = P::width(pc), base_ch = P::base(pc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < w / 16; ++e)
+            buf[wave][j][base_ch + (4 * h + i) * (w / 16) + e] = acc[m][base_ch / 16 + e][i];
+      });
+      __syncthreads();
+      for (int i = tid; i < 16 * (D / 4); i += kAttendThreads) {
+        const int rr = i / (D / 4), ch = (i - rr * (D / 4)) * 4;
+        uint32_t g = (uint32_t)(row0 + 16 * m + rr);
+        if ((int)g >= A.rows) continue;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[w][rr].x);
+        float total = 0.f;
+        f4 o{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float f = stat[w][rr].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[w][rr].x - top);
+          // (a wave that saw nothing has no part, and a sum of one that is not a number stays)
+          total += stat[w][rr].y * f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += buf[w][rr][ch + e] * f;
+        }
+        if (!complete) {
+          const int64_t at = (int64_t)slot * (16 * MT) + 16 * m + rr;
+          *(f4*)(A.sums + at * D + ch) = o;
+          if (ch == 0) A.stats[at] = make_float2(top, total);
+        } else {
+          const int r = (int)A.by_group.split(g);
+          finish<DT>(A, b, r, head * A.group + (int)g, D, ch, r < range.fresh ? top : -INFINITY,
+                     r < range.fresh ? total : 0.f, o);
+        }
+      }
+    }
+  }
+}
+
+// Joins what several workgroups have of a run, a wave for each row; rows of requests
+// that have no unit are zero.
+template <int DT, int D, int MT>
+__global__ __launch_bounds__(kAttendThreads) void join_kernel(AttendArgs A) {
+  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;      // of a row, and rows' parts at once
+  const int lane = threadIdx.x & 63;
+  const int heads = A.a.cache.heads;
+  uint32_t g = blockIdx.x * (kAttendThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = (int)(g / (uint32_t)(heads * A.rows));
+  if (b >= A.a.B) return;
+  g -= (uint32_t)b * (uint32_t)(heads * A.rows);
+  const int head = (int)(g / (uint32_t)A.rows), row = (int)g - head * A.rows;
+  const int start = A.starts[b], all = A.starts[A.a.B];
+  const int n = (A.starts[b + 1] - start) / (heads * A.row_tiles);
+  g = (uint32_t)row;
+  const int r = (int)A.by_group.split(g), q_head = head * A.group + (int)g;
+  const int group = lane / kLanes, ch = (lane - group * kLanes) * 4;
+  const bool first = lane < kLanes;
+  if (n == 0) {
+    if (first) finish<DT>(A, b, r, q_head, D, ch, -INFINITY, 0.f, f4{0, 0, 0, 0});
+    return;
+  }
+  const int G = min(A.workgroups, all);
+  const long long u0 = start + (long long)(head * A.row_tiles + row / (16 * MT)) * n;
+  // the workgroups of units u0 and u0 + n - 1: the last w with w all / G <= u
+  const int w0 = (int)(((u0 + 1) * G - 1) / all), w1 = (int)(((u0 + n) * G - 1) / all);
+  if (w0 == w1) return;
+  // (a workgroup's second place is that of a run that it begins)
+  const bool begins = (long long)w0 * all / G <= u0;
+  auto place = [&](int w) { return (int64_t)(2 * w + (w == w0 && begins ? 1 : 0)) * (16 * MT) + row % (16 * MT); };
+  float top = -INFINITY;
+  for (int w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, A.stats[place(w)].x);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  float total = 0.f;
+  f4 o{0, 0, 0, 0};
+  if (group < kGroups) {
+    for (int w = w0 + group; w <= w1; w += kGroups) {
+      const float2 st = A.stats[place(w)];
+      const f4 x = *(const f4*)(A.sums + place(w) * D + ch);
+      const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
+      total += st.y * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < kGroups; ++k) {
+    const int from = (lane + k * kLanes) & 63;
+    const float t = __shfl(total, from);
+    f4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __shfl(o[e], from);
+    if (first) {
+      total += t;
+      // (sums of the first lanes' own, which later groups do not read)
+      o += x;
+    }
+  }
+  if (!first) return;
+  const Range range(A, b);
+  const bool is = r < range.fresh;
+  finish<DT>(A, b, r, q_head, D, ch, is ? top : -INFINITY, is ? total : 0.f, o);
+}
+
+}  // namespace asym_cache
+
+#endif  // ASYMSPEC_CACHE_ATTEND_H_

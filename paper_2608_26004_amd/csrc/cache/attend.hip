@@ -1,0 +1,45 @@
+// The kernels of attend_cache for one width of codes, type of queries and kind of
+// block size.
+
+#include <hip/hip_runtime.h>
+
+#include "../step/launch.h"
+#include "attend.h"
+#include "attend_host.h"
+
+namespace asym_cache {
+
+constexpr int kBits = ASYMSPEC_PART_BITS, kType = ASYMSPEC_PART_DT;
+constexpr bool kWhole = ASYMSPEC_PART_WHOLE != 0;
+
+template <int D, int MT>
+static int attend_launch(AttendArgs& A, void* stream) {
+  const int rc = asym_step::launch(attend_kernel<kBits, kType, D, MT, kWhole>, (unsigned)A.workgroups, kAttendThreads, 0,
+                                   stream, A);
+  if (rc != ASYMSPEC_OK) return rc;
+  const long long rows = (long long)A.a.B * A.a.cache.heads * A.rows;
+  return asym_step::launch(join_kernel<kType, D, MT>, (unsigned)((rows + 3) / 4), kAttendThreads, 0, stream, A);
+}
+
+template <int D>
+static int attend_tiles(AttendArgs& A, int tiles, void* stream) {
+  constexpr int kMost = attend_most_tiles(kType == ASYMSPEC_BF16, D);
+  if constexpr (kMost >= 4)
+    if (tiles == 4) return attend_launch<D, 4>(A, stream);
+  if constexpr (kMost >= 2)
+    if (tiles == 2) return attend_launch<D, 2>(A, stream);
+  return attend_launch<D, 1>(A, stream);
+}
+
+template <>
+int attend_part<kBits, kType, kWhole>(AttendArgs& A, int tiles, void* stream) {
+  switch (A.a.cache.dim) {
+    case 64: return attend_tiles<64>(A, tiles, stream);
+    case 96: return attend_tiles<96>(A, tiles, stream);
+    case 128: return attend_tiles<128>(A, tiles, stream);
+    case 192: return attend_tiles<192>(A, tiles, stream);
+    default: return attend_tiles<256>(A, tiles, stream);
+  }
+}
+
+}  // namespace asym_cache

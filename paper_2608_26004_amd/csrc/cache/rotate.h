@@ -1,0 +1,109 @@
+// rotate_heads: a workgroup takes a few tokens, computes each angle's sine and cosine
+// once into LDS, and turns the channels of all their heads with them.
+
+#ifndef ASYMSPEC_CACHE_ROTATE_H_
+#define ASYMSPEC_CACHE_ROTATE_H_
+
+#include "format.h"
+
+namespace asym_cache {
+
+constexpr int kRotateThreads = 256;
+constexpr int kRotateMostTokens = 8;
+
+struct RotateArgs {
+  asymspec_rotate r;
+  uint32_t tokens;          // B * R
+  int T;                    // tokens of a workgroup
+  uint32_t pieces, tail;    // of a head: all, and those that are only copied
+  Div by_n, by_R, by_pieces, by_heads;
+};
+
+// VEC: pieces of 16 bytes of each of the pair's sides (or of both, interleaved);
+// else of one pair.
+template <int DT, bool INTER, bool VEC>
+__global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs A) {
+  typedef typename Row<DT>::T T;
+  constexpr int VE = VEC ? Row<DT>::VE : 1;
+  extern __shared__ float2 turn[];                       // [T][n]
+  const asymspec_rotate& r = A.r;
+  const uint32_t first = blockIdx.x * (uint32_t)A.T;
+  const uint32_t here = min((uint32_t)A.T, A.tokens - first);
+  for (uint32_t i = threadIdx.x; i < here * (uint32_t)r.n; i += kRotateThreads) {
+    uint32_t f = i;
+    const uint32_t token = first + A.by_n.split(f);
+    uint32_t row = token;
+    const uint32_t b = A.by_R.split(row);
+    const long long p = r.every_row ? (long long)r.positions[token] : (long long)r.positions[b] + row;
+    // in turns: the whole ones leave in 64 bits, what stays is exact to 2^-24 of a turn
+    // and better
+    double t = (double)p * (r.frequencies[f] * 0.15915494309189533577);
+    t -= rint(t);
+    float s, c;
+    sincospif(2.0f * (float)t, &s, &c);
+    turn[i] = make_float2(c * r.magnitude, s * r.magnitude);
+  }
+  __syncthreads();
+  const uint32_t heads = (uint32_t)(r.q_heads + r.k_heads);
+  const uint32_t all = here * heads * A.pieces;
+  const uint32_t turned = A.pieces - A.tail;
+  for (uint32_t i = threadIdx.x; i < all; i += kRotateThreads) {
+    uint32_t piece = i;
+    uint32_t head = A.by_pieces.split(piece);
+    const uint32_t t = A.by_heads.split(head);
+    uint32_t row = first + t;
+    const uint32_t b = A.by_R.split(row);
+    const bool is_q = head < (uint32_t)r.q_heads;
+    if (!is_q) head -= (uint32_t)r.q_heads;
+    const asymspec_heads& x = is_q ? r.q : r.k;
+    const asymspec_heads& y = is_q ? r.q_out : r.k_out;
+    const T* in = (const T*)x.at + (b * x.request + row * x.row + head * x.head);
+    T* out = (T*)y.at + (b * y.request + row * y.row + head * y.head);
+    const float2* w = turn + t * (uint32_t)r.n;
+    if (piece >= turned) {
+      const uint32_t c = 2u * (uint32_t)r.n + (piece - turned) * VE;
+      if constexpr (VEC) asym_step::store_vec<DT>(out + c, asym_step::load_vec<DT>(in + c));
+      else out[c] = in[c];
+    } else if constexpr (INTER) {
+      if constexpr (VEC) {
+        u4 v = asym_step::load_vec<DT>(in + piece * VE);
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+          const float2 cs = w[(piece * VE + e) / 2];
+          const float p = Row<DT>::get(v, e), q = Row<DT>::get(v, e + 1);
+          Row<DT>::put(v, e, p * cs.x - q * cs.y);
+          Row<DT>::put(v, e + 1, p * cs.y + q * cs.x);
+        }
+        asym_step::store_vec<DT>(out + piece * VE, v);
+      } else {
+        const float2 cs = w[piece];
+        const float p = Row<DT>::get1(in[2 * piece]), q = Row<DT>::get1(in[2 * piece + 1]);
+        out[2 * piece] = Row<DT>::put1(p * cs.x - q * cs.y);
+        out[2 * piece + 1] = Row<DT>::put1(p * cs.y + q * cs.x);
+      }
+    } else {
+      const uint32_t c = piece * VE;
+      if constexpr (VEC) {
+        u4 v = asym_step::load_vec<DT>(in + c), z = asym_step::load_vec<DT>(in + c + r.n);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float2 cs = w[c + e];
+          const float p = Row<DT>::get(v, e), q = Row<DT>::get(z, e);
+          Row<DT>::put(v, e, p * cs.x - q * cs.y);
+          Row<DT>::put(z, e, p * cs.y + q * cs.x);
+        }
+        asym_step::store_vec<DT>(out + c, v);
+        asym_step::store_vec<DT>(out + c + r.n, z);
+      } else {
+        const float2 cs = w[c];
+        const float p = Row<DT>::get1(in[c]), q = Row<DT>::get1(in[c + r.n]);
+        out[c] = Row<DT>::put1(p * cs.x - q * cs.y);
+        out[c + r.n] = Row<DT>::put1(p * cs.y + q * cs.x);
+      }
+    }
+  }
+}
+
+}  // namespace asym_cache
+
+#endif  // ASYMSPEC_CACHE_ROTATE_H_

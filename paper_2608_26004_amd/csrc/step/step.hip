@@ -4,54 +4,17 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <atomic>
 #include <cstdint>
-#include <cstring>
 
 #include "asymspec_step.h"
 #include "commit.h"
 #include "draw.h"
+#include "launch.h"
 #include "shape.h"
 #include "slots.h"
 #include "span.h"
 
 namespace asym_step {
-
-static bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
-// Compute units of the current device, or 0 when it is no gfx950.
-static int device_cus() {
-  static std::atomic<int> cus[64];       // 0: not looked at; -1: not a gfx950
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) {
-    (void)hipGetLastError();
-    return 0;
-  }
-  int n = cus[dev].load(std::memory_order_relaxed);
-  if (n == 0) {
-    hipDeviceProp_t pr;
-    if (hipGetDeviceProperties(&pr, dev) != hipSuccess) {
-      (void)hipGetLastError();
-      return 0;
-    }
-    n = std::strncmp(pr.gcnArchName, "gfx950", 6) == 0 ? pr.multiProcessorCount : -1;
-    cus[dev].store(n, std::memory_order_relaxed);
-  }
-  return std::max(n, 0);
-}
-
-// A launch has fewer than 2^32 threads.
-static bool fits(long long grid, int threads) { return grid <= 0xFFFFFFFFll / threads; }
-
-// Enqueues a kernel of one argument.
-template <class Args>
-static int launch(void (*kernel)(Args), unsigned grid, int threads, size_t lds, void* stream, Args& args) {
-  void* p[] = {&args};
-  if (hipLaunchKernel((const void*)kernel, dim3(grid), dim3(threads), p, lds, (hipStream_t)stream) == hipSuccess)
-    return ASYMSPEC_OK;
-  (void)hipGetLastError();
-  return ASYMSPEC_E_DEVICE;
-}
 
 // Elements from the first to behind the last of a [B][R][V] tensor, or -1 when a
 // stride is negative or the tensor larger than any memory.

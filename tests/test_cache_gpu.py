@@ -1,0 +1,562 @@
+"""The operators of a quantised paged cache on the GPU, against the plain references
+of cache_ref.py (64 bits)."""
+
+import math
+
+import numpy as np
+import pytest
+
+import paper_2608_26004_amd as asp
+
+import cache_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+HALF = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}     # half a step, relative
+TINY = {"bf16": 2.0 ** -133, "fp32": 2.0 ** -149}
+
+
+def gpu(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def i32(x):
+    return np.asarray(x, np.int32)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def stored(rng, shape, dtype, scale=1.0):
+    return torch.from_numpy((scale * rng.standard_normal(shape)).astype(np.float32)).cuda().to(DT[dtype])
+
+
+# ------------------------------------------------------------------- rotate --
+def rotated(x, positions, f, interleaved, magnitude):
+    """(fp64 rotation, bound on an fp32 evaluation's error) of x [B, R, H, D]."""
+    n = len(f)
+    a = positions.astype(np.float64)[..., None] * f
+    cos, sin = (g(a)[:, :, None] * magnitude for g in (np.cos, np.sin))
+    y = x.copy()
+    p, q = (x[..., 0:2 * n:2], x[..., 1:2 * n:2]) if interleaved else (x[..., :n], x[..., n:2 * n])
+    c, d = p * cos - q * sin, p * sin + q * cos
+    # the angle: three roundings in 64 bits here and there, one to fp32 of at most half
+    # a turn; sine and cosine within 2 units; magnitude, two products and a sum
+    e = np.abs(a)[:, :, None] * 6 * 2.0 ** -53 + 2 * math.pi * 2.0 ** -26 + 4 * 2.0 ** -24
+    err = np.zeros_like(x)
+    size = (np.abs(p) + np.abs(q)) * abs(magnitude) * (e + 4 * 2.0 ** -24)
+    for out, val in ((y, (c, d)), (err, (size, size))):
+        if interleaved:
+            out[..., 0:2 * n:2], out[..., 1:2 * n:2] = val
+        else:
+            out[..., :n], out[..., n:2 * n] = val
+    return y, err
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,R,H,Hk,D,n,interleaved", [
+    (1, 1, 1, 1, 64, 32, False), (3, 5, 8, 2, 128, 64, False), (2, 3, 4, 4, 96, 24, True), (5, 1, 3, 1, 80, 13, False),
+    (2, 7, 6, 3, 34, 17, True), (1, 2, 2, 1, 2, 1, False), (300, 4, 4, 2, 128, 16, False), (1200, 1, 2, 2, 256, 128, True),
+    (4, 2, 5, 1, 1024, 512, False), (2, 2, 3, 1, 100, 8, True)])
+def test_rotate(dtype, B, R, H, Hk, D, n, interleaved):
+    rng = np.random.default_rng(B * 1000 + D + n)
+    qkv = stored(rng, (B, R, H + 2 * Hk, D), dtype, 2.0)
+    q, k = qkv[:, :, :H], qkv[:, :, H:H + Hk]
+    pos = i32(rng.integers(-50, 200000, B))
+    pos[0] = 2 ** 31 - 1 if B > 1 else 77
+    f = 10000.0 ** (-np.arange(n) / n)
+    for every in (False, True):
+        p = pos[:, None].astype(np.int64) + np.arange(R)
+        given = pos
+        if every:
+            p = rng.integers(-2 ** 31, 2 ** 31, (B, R))
+            given = i32(p)
+        got = asp.rotate_heads(q, k, gpu(given), gpu(f), interleaved=interleaved, magnitude=1.25)
+        for x, y in zip((q, k), got):
+            want, err = rotated(f64(x), p, f, interleaved, 1.25)
+            assert y.is_contiguous() and y.dtype == x.dtype
+            off = np.abs(f64(y) - want)
+            assert (off <= err + HALF[dtype] * np.abs(want) + TINY[dtype]).all(), (every, off.max())
+            assert torch.equal(y[..., 2 * n:], x[..., 2 * n:])
+    # in place, within the projection: the values' heads stay
+    whole = qkv.clone()
+    a, b = whole[:, :, :H], whole[:, :, H:H + Hk]
+    ra, rb = asp.rotate_heads(a, b, gpu(given), gpu(f), interleaved=interleaved, magnitude=1.25, out=(a, b))
+    assert ra is a and rb is b
+    assert torch.equal(a, got[0]) and torch.equal(b, got[1]) and torch.equal(whole[:, :, H + Hk:], qkv[:, :, H + Hk:])
+    alone = asp.rotate_heads(q, None, gpu(given), gpu(f), interleaved=interleaved, magnitude=1.25)
+    assert torch.equal(alone, got[0])
+
+
+def test_rotate_heads_major_and_other_outputs():
+    """Heads outside rows, requests in no order of memory, and outputs of other strides."""
+    rng = np.random.default_rng(5)
+    x = stored(rng, (4, 6, 3, 64), "bf16")                 # [B][heads][R][D]
+    q, k = x[:, :4].transpose(1, 2), x[:, 4:].transpose(1, 2)
+    pos, f = gpu(i32([3, 9, 0, 100])), gpu(10000.0 ** (-np.arange(32) / 32))
+    want = asp.rotate_heads(q.contiguous(), k.contiguous(), pos, f)
+    got = asp.rotate_heads(q, k, pos, f)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    out = torch.full((3, 4, 9, 70), 7.0, dtype=torch.bfloat16, device="cuda")      # [R][B][heads][..]
+    o = out.transpose(0, 1)
+    got = asp.rotate_heads(q, k, pos, f, out=(o[:, :, :4, 3:67], o[:, :, 5:7, :64]))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    assert (out[..., 4, :] == 7).all() and (out[..., 7:, :] == 7).all() and (out[..., 67:] == 7).all()
+    # in place in the tensor that holds both
+    y = x.clone()
+    a, b = y[:, :4].transpose(1, 2), y[:, 4:].transpose(1, 2)
+    asp.rotate_heads(a, b, pos, f, out=(a, b))
+    assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+def test_rotate_back():
+    """Positions below zero turn back what those above turned, but for the roundings."""
+    rng = np.random.default_rng(6)
+    q = stored(rng, (3, 2, 2, 128), "fp32")
+    f = asp.rotary_frequencies(128)
+    pos = i32([[5, 100000], [7, 8], [1 << 20, 3]])
+    there = asp.rotate_heads(q, None, gpu(pos), f)
+    back = asp.rotate_heads(there, None, gpu(-pos), f)
+    # two rotations, each within (|x| + |y|) (2 pi 2^-26 + 8 * 2^-24) and half a step
+    size = f64(q).reshape(3, 2, 2, 2, 64)
+    size = np.abs(size).sum(3, keepdims=True).repeat(2, 3).reshape(q.shape)
+    assert (np.abs(f64(back) - f64(q)) <= 2 * 2 * size * (2 * math.pi * 2.0 ** -26 + 9 * 2.0 ** -24)).all()
+
+
+# -------------------------------------------------------------------- write --
+def empty(blocks, heads, S, D, bits, fill=None, rng=None):
+    shapes = [(blocks, heads, S, D * bits // 8), (blocks, heads, S, D // 32)] * 2
+    if rng is not None:
+        return [rng.integers(0, 256, s, dtype=np.uint8) for s in shapes]
+    return [np.full(s, fill or 0, np.uint8) for s in shapes]
+
+
+def on_gpu(cache):
+    return tuple(gpu(x) for x in cache)
+
+
+def assert_cache(got, want):
+    for name, a, b in zip(("keys", "key_scales", "values", "value_scales"), got, want):
+        a = a.cpu().numpy()
+        assert np.array_equal(a, b), (name, np.argwhere(a != b)[:5], a[a != b][:5], b[a != b][:5])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("tokens,heads,D,S", [(1, 1, 32, 1), (5, 3, 64, 16), (17, 2, 96, 7), (33, 5, 128, 32),
+                                              (16, 8, 256, 16), (50, 1, 192, 24), (300, 4, 160, 16)])
+def test_write(dtype, bits, tokens, heads, D, S):
+    rng = np.random.default_rng(tokens * 7 + D)
+    N = 2 * tokens // S + 3
+    want = empty(N, heads, S, D, bits, rng=rng)           # what is not written stays
+    cache = on_gpu(want)
+    slots = rng.permutation(N * S)[:tokens].astype(np.int64)
+    for i, s in ((0, -1), (2, N * S), (3, -2 ** 40), (4, 2 ** 40)):
+        if tokens > 4:
+            slots[i] = s
+    kv = rng.standard_normal((tokens, 2 * heads, D)) * 10.0 ** rng.integers(-6, 6, (tokens, 2 * heads, 1))
+    kv = torch.from_numpy(kv.astype(np.float32)).cuda().to(DT[dtype])
+    k, v = kv[:, :heads], kv[:, heads:]
+    assert asp.write_cache(k, v, gpu(slots), cache) is cache
+    ref.write(want, f64(k), f64(v), slots, bits)
+    assert_cache(cache, want)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_write_every_code_and_halfway(bits):
+    """Values on, beside and halfway between the codes, at scales from the smallest on."""
+    lv = ref.levels(bits)
+    mid = (lv[1:] + lv[:-1]) / 2
+    vals = np.concatenate([lv, mid, mid * (1 + 2.0 ** -20), mid * (1 - 2.0 ** -20)])
+    vals = np.concatenate([vals, -vals])
+    rows = []
+    for e in (-100, -99, -20, 0, 13, 119 if bits == 8 else 124):
+        for lo in range(0, len(vals), 31):
+            x = np.full(32, lv[-1])                        # keeps the scale
+            x[1:1 + len(vals[lo:lo + 31])] = vals[lo:lo + 31]
+            rows.append(x * 2.0 ** e)
+    x = np.zeros((len(rows), 1, 32), np.float32)
+    x[:, 0] = np.array(rows, np.float32)
+    for dtype in ("fp32", "bf16"):
+        t = torch.from_numpy(x).cuda().to(DT[dtype])
+        want = empty(len(rows), 1, 1, 32, bits)
+        cache = on_gpu(want)
+        slots = np.arange(len(rows), dtype=np.int64)
+        asp.write_cache(t, -t, gpu(slots), cache)
+        ref.write(want, f64(t), -f64(t), slots, bits)
+        assert_cache(cache, want)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_write_all_bf16_values(bits):
+    """Each bf16 number as the largest of a block of its fractions, among them the
+    infinities, those that are not a number, zeros and what is below the smallest scale."""
+    b = np.arange(1 << 16, dtype=np.int64)
+    x = torch.from_numpy(b.astype(np.uint16).view(np.int16)).cuda().view(torch.bfloat16)
+    frac = torch.linspace(-1, 1, 32, device="cuda")
+    frac[31] = 1.0
+    t = (x.float()[:, None] * frac).to(torch.bfloat16)
+    t[:, 31] = x
+    t = t[:, None]
+    want = empty(1 << 12, 1, 16, 32, bits)
+    cache = on_gpu(want)
+    asp.write_cache(t, t.float().flip(0).to(torch.bfloat16), gpu(b), cache)
+    with np.errstate(all="ignore"):
+        k = f64(t)
+        for part, y in ((0, k), (2, k[::-1])):
+            codes, scales = ref.encode(y, bits)
+            want[part][:] = ref.packed(codes, bits).reshape(want[part].shape[:1] + (16, 1, -1)).transpose(0, 2, 1, 3)
+            want[part + 1][:] = scales.reshape(1 << 12, 16, 1, 1).transpose(0, 2, 1, 3)
+    assert_cache(cache, want)
+
+
+# --------------------------------------------------------------------- read --
+def tables(rng, lengths, S, N, extra=2):
+    """Block tables of distinct blocks in no order, and how many blocks are taken."""
+    need = [-(-max(0, int(n)) // S) for n in lengths]
+    ids = rng.permutation(N)[:sum(need)]
+    t = np.full((len(lengths), max(need) + extra), -1)
+    at = 0
+    for b, n in enumerate(need):
+        t[b, :n] = ids[at:at + n]
+        at += n
+    return i32(t)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("B,heads,D,S,L", [(1, 1, 32, 1, 1), (3, 2, 64, 16, 40), (4, 3, 96, 7, 33), (2, 8, 128, 32, 100),
+                                           (3, 1, 256, 24, 50)])
+def test_read(dtype, bits, B, heads, D, S, L):
+    rng = np.random.default_rng(B + D)
+    N = B * (L // S + 2) + 4
+    cache = empty(N, heads, S, D, bits, rng=rng)
+    for p in (1, 3):                                       # bytes that are written, and 255
+        cache[p] = np.where(rng.random(cache[p].shape) < 0.02, 255, rng.integers(100, 150, cache[p].shape)).astype(np.uint8)
+    lengths = i32(rng.integers(0, L + 1, B))
+    lengths[-1] = L
+    table = tables(rng, lengths, S, N)
+    if B > 2:
+        table[1, 0] = N + 5                                # blocks that are not there
+        lengths[0] = -3
+    first = i32(rng.integers(-3, L // 2 + 1, B))
+    got_cache = on_gpu(cache)
+    for f in (None, first):
+        k, v = asp.read_cache(got_cache, gpu(table), gpu(lengths), L + 3, first=gpu(f), dtype=DT[dtype])
+        for got, want in zip((k, v), ref.read(cache, table, lengths, L + 3, f, bits)):
+            assert got.shape == (B, L + 3, heads, D) and got.dtype == DT[dtype]
+            assert np.array_equal(f64(got), want, equal_nan=True)
+    o = (torch.empty_like(k), torch.empty_like(v))
+    assert asp.read_cache(got_cache, gpu(table), gpu(lengths), L + 3, first=gpu(first), dtype=DT[dtype], out=o)[0] is o[0]
+    assert all(torch.equal(a.nan_to_num(7), b.nan_to_num(7)) for a, b in zip(o, (k, v)))
+
+
+# ------------------------------------------------------------------- attend --
+def attend_inputs(rng, B, R, H, Hk, D, bits, S, dtype, lengths, garbage=True):
+    """Queries, a cache (as arrays) that holds the requests' positions and garbage
+    everywhere else, the tables, and spare blocks that nobody has."""
+    need = [max(0, int(n)) + R for n in lengths]
+    N = sum(-(-n // S) for n in need) + 3
+    cache = empty(N, Hk, S, D, bits, rng=rng) if garbage else empty(N, Hk, S, D, bits)
+    table = tables(rng, need, S, N, extra=1)
+    for b, n in enumerate(need):
+        p = np.arange(n)
+        slots = table[b, p // S].astype(np.int64) * S + p % S
+        k = rng.standard_normal((n, Hk, D)) * np.exp(0.5 * rng.standard_normal((Hk, D)))
+        ref.write(cache, k, rng.standard_normal((n, Hk, D)), slots, bits)
+    q = stored(rng, (B, R, H + 2, D), dtype, 1.5)[:, :, 1:H + 1]
+    return q, cache, table
+
+
+def check_attend(q, cache, table, lengths, bits, new_tokens=None, scale=None, window=0):
+    dtype = "bf16" if q.dtype == torch.bfloat16 else "fp32"
+    out, lse = asp.attend_cache(q, on_gpu(cache), gpu(table), gpu(i32(lengths)),
+                                new_tokens=None if new_tokens is None else gpu(i32(new_tokens)), scale=scale,
+                                window=window, return_lse=True)
+    # the formula's scale as the kernel has it, in fp32
+    at = float(np.float32(scale if scale is not None else q.shape[-1] ** -0.5))
+    x = f64(q)
+    if dtype == "bf16":
+        x = x.astype(np.float32)                           # (exact; its type says how a probability is split)
+    want, wlse, err, lerr = ref.attend(x, cache, table, lengths, new_tokens, at, window, bits)
+    got, glse = f64(out), f64(lse)
+    for a, e in ((got, err), (glse, lerr), (want, err), (wlse, lerr)):
+        a[np.isinf(e)] = 0.0                               # (beyond fp32: anything)
+    nan = np.isnan(want)
+    assert np.array_equal(np.isnan(got), nan), (np.argwhere(np.isnan(got) != nan)[:5])
+    assert np.array_equal(np.isnan(glse), np.isnan(wlse)) and np.array_equal(np.isinf(glse), np.isinf(wlse))
+    # (c = scale * log2 e is rounded once more: a relative 2^-24 of the scores, as their bound has)
+    ok = np.abs(got - want) <= err + HALF[dtype] * (np.abs(want) + err) + TINY[dtype]
+    assert (ok | nan).all(), (np.abs(got - want)[~(ok | nan)][:5], err[~(ok | nan)][:5], np.argwhere(~(ok | nan))[:5])
+    fin = np.isfinite(wlse)
+    assert (np.abs(glse[fin] - wlse[fin]) <= lerr[fin]).all(), (np.abs(glse[fin] - wlse[fin]).max(), lerr[fin].max())
+    alone = asp.attend_cache(q, on_gpu(cache), gpu(table), gpu(i32(lengths)),
+                             new_tokens=None if new_tokens is None else gpu(i32(new_tokens)), scale=scale, window=window)
+    assert torch.equal(alone.nan_to_num(7), out.nan_to_num(7))
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("S", [16, 7])
+def test_attend_dims(dtype, bits, D, S):
+    """Every instance's one row tile, then several, then several groups of them."""
+    rng = np.random.default_rng(D + S)
+    for B, R, H, Hk in ((2, 1, 2, 1), (2, 3, 8, 1), (1, 5, 24, 2), (1, 9, 8, 1)):
+        lengths = rng.integers(0, 300, B)
+        q, cache, table = attend_inputs(rng, B, R, H, Hk, D, bits, S, dtype, lengths)
+        check_attend(q, cache, table, lengths, bits)
+
+
+@pytest.mark.parametrize("bits,S,dtype", [(4, 16, "bf16"), (8, 32, "bf16"), (4, 1, "fp32"), (8, 24, "fp32"), (4, 128, "bf16")])
+@pytest.mark.parametrize("window", [0, 1, 37, 200])
+def test_attend_lengths(bits, S, dtype, window):
+    """Lengths of none, one and those around the sizes of units, waves and blocks, with
+    fewer rows for some requests, all in one call; negative and far too large ones."""
+    rng = np.random.default_rng(window + S)
+    lengths = np.array([0, 1, 15, 16, 31, 32, 33, 127, 128, 129, 255, 300, 2, 511, 640])
+    R = 3
+    new = rng.integers(-1, R + 2, len(lengths))
+    new[:3], new[12] = R, 0
+    q, cache, table = attend_inputs(rng, len(lengths), R, 4, 2, 64, bits, S, dtype, lengths)
+    check_attend(q, cache, table, lengths, bits, new_tokens=new, window=window)
+    table[3, 0] = -1                                       # blocks that are not there
+    table[6, -2:] = cache[0].shape[0]
+    table[11] = -7
+    far = lengths.copy()
+    far[4], far[5], far[8] = -9, 700, 2 ** 31 - 1
+    check_attend(q, cache, table, far, bits, new_tokens=new, window=window)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("R,H,Hk", [(64, 2, 2), (17, 5, 1), (1, 64, 1), (9, 14, 2), (33, 1, 1)])
+def test_attend_rows(bits, R, H, Hk):
+    rng = np.random.default_rng(R)
+    lengths = [0, 100]
+    q, cache, table = attend_inputs(rng, 2, R, H, Hk, 64, bits, 16, "bf16", lengths)
+    check_attend(q, cache, table, lengths, bits)
+    q, cache, table = attend_inputs(rng, 2, R, H, Hk, 128, bits, 16, "bf16", lengths)
+    check_attend(q, cache, table, lengths, bits, window=50)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("S", [16, 5])
+def test_attend_not_finite(bits, dtype, S):
+    """A key that is not finite is felt by the rows that see it, in all channels; a value
+    in the 32 channels of its scale; and neither by rows that do not see it."""
+    rng = np.random.default_rng(S)
+    lengths, R = [40, 130, 7, 260], 4
+    q, cache, table = attend_inputs(rng, 4, R, 4, 2, 128, bits, S, dtype, lengths)
+
+    def at(b, p):
+        return table[b, p // S], p % S
+    a = at(0, 42)                                          # rows 2 and 3
+    cache[1][a[0], 1, a[1], 2] = 255
+    a = at(1, 132)                                         # a value, rows 2 and 3
+    cache[3][a[0], 0, a[1], 1] = 255
+    a = at(2, 10)                                          # the last row alone
+    cache[3][a[0], 1, a[1], 3] = 255
+    a = at(3, 11)                                          # seen by all without a window
+    cache[3][a[0], 1, a[1], 0] = 255
+    if bits == 8:                                          # a code that is not a number
+        a = at(1, 131)
+        cache[2][a[0], 1, a[1], 77] = 0x7F
+        a = at(2, 3)
+        cache[0][a[0], 0, a[1], 5] = 0xFF
+    for window in (0, 2, 250):
+        out, _ = check_attend(q, cache, table, lengths, bits, window=window)
+        assert bool(out.isnan().any())
+
+
+def test_attend_extremes():
+    """Scores far from zero, equal ones, a scale of zero, and a negative one."""
+    rng = np.random.default_rng(3)
+    lengths = [200, 3]
+    q, cache, table = attend_inputs(rng, 2, 2, 4, 2, 64, 4, 16, "fp32", lengths)
+    for scale in (0.0, -0.3, 20.0, 1e-6):
+        check_attend(q, cache, table, lengths, 4, scale=scale)
+    check_attend(q * 0, cache, table, lengths, 4)
+
+
+@pytest.mark.parametrize("bits,S", [(4, 16), (8, 64), (4, 24)])
+def test_attend_long(bits, S):
+    """Requests of very different lengths, cut over many workgroups."""
+    rng = np.random.default_rng(bits)
+    lengths = [9000, 0, 1, 5000, 130]
+    q, cache, table = attend_inputs(rng, 5, 2, 4, 2, 64, bits, S, "bf16", lengths, garbage=False)
+    check_attend(q, cache, table, lengths, bits)
+    check_attend(q, cache, table, lengths, bits, window=3000, new_tokens=[2, 1, 2, 0, 1])
+
+
+def test_attend_many_requests():
+    rng = np.random.default_rng(9)
+    B = 700
+    lengths = rng.integers(0, 40, B)
+    q, cache, table = attend_inputs(rng, B, 1, 2, 1, 64, 4, 16, "bf16", lengths)
+    check_attend(q, cache, table, lengths, 4)
+
+
+def test_attend_offsets_beyond_32_bits():
+    """Blocks whose codes begin beyond 2^32 bytes."""
+    S, D, bits = 64, 256, 8
+    N = (1 << 32) // (S * D) + 40
+    rng = np.random.default_rng(4)
+    small = attend_inputs(rng, 1, 2, 4, 1, D, bits, S, "bf16", [600])
+    q, cache, table = small
+    big = asp.new_cache(N, 1, S, D, bits)
+    n = cache[0].shape[0]
+    for x, y in zip(big, cache):
+        x[N - n:] = gpu(y)
+    want = asp.attend_cache(q, on_gpu(cache), gpu(table), gpu(i32([600])))
+    moved = np.where(table >= 0, table + N - n, -1).astype(np.int32)
+    got = asp.attend_cache(q, big, gpu(moved), gpu(i32([600])))
+    assert torch.equal(got, want)
+    k, v = asp.read_cache(big, gpu(moved), gpu(i32([602])), 602)
+    k2, v2 = asp.read_cache(on_gpu(cache), gpu(table), gpu(i32([602])), 602)
+    assert torch.equal(k, k2) and torch.equal(v, v2)
+    slots = torch.tensor([[N * S - 1]], device="cuda")
+    x = stored(rng, (1, 1, 1, D), "bf16")
+    asp.write_cache(x, x, slots, big)
+    one = asp.new_cache(1, 1, 1, D, bits)
+    asp.write_cache(x, x, slots * 0, one)
+    assert all(torch.equal(a[-1, 0, -1], b[0, 0, 0]) for a, b in zip(big, one))
+
+
+# ----------------------------------------------------------------- together --
+def step_state(rng, B, R, H, Hk, D, bits, S, pool):
+    dev = "cuda"
+    s = dict(cache=asp.new_cache(pool, Hk, S, D, bits), table=torch.full((B, pool // 2), -1, dtype=torch.int32, device=dev),
+             held=torch.zeros(B, dtype=torch.int32, device=dev), ring=torch.arange(pool, dtype=torch.int32, device=dev),
+             free=torch.tensor([0, pool], dtype=torch.int32, device=dev), lengths=torch.zeros(B, dtype=torch.int32, device=dev))
+    return s
+
+
+def run_step(s, qkv, H, Hk, f, S):
+    """One layer's step: slots, rotation, write and answer, all on the device."""
+    R = qkv.shape[1]
+    slots, short, s["held"], s["free"] = asp.plan_slots(s["lengths"], None, s["table"], s["held"], s["ring"], s["free"], S,
+                                                        width=R)
+    q, k = asp.rotate_heads(qkv[:, :, :H], qkv[:, :, H:H + Hk], s["lengths"], f)
+    asp.write_cache(k, qkv[:, :, H + Hk:], slots, s["cache"])
+    return asp.attend_cache(q, s["cache"], s["table"], s["lengths"], return_lse=True) + (short,)
+
+
+def test_steps_together():
+    """Steps of drafts of which some are rejected, over plan_slots' tables, against dense
+    attention in 64 bits over the keys and values that were kept."""
+    rng = np.random.default_rng(1)
+    B, R, H, Hk, D, bits, S = 3, 3, 4, 2, 64, 8, 4
+    s = step_state(rng, B, R, H, Hk, D, bits, S, 64)
+    f = asp.rotary_frequencies(D)
+    fn = f.cpu().numpy()
+    kept = [[] for _ in range(B)]
+    for step in range(12):
+        qkv = stored(rng, (B, R, H + 2 * Hk, D), "bf16")
+        out, lse, short = run_step(s, qkv, H, Hk, f, S)
+        assert not short.any()
+        n = s["lengths"].cpu().numpy()
+        pos = n[:, None] + np.arange(R)
+        q, k = asp.rotate_heads(qkv[:, :, :H], qkv[:, :, H:H + Hk], gpu(i32(pos)), f)
+        want_q, err = rotated(f64(qkv[:, :, :H]), pos, fn, False, 1.0)
+        assert (np.abs(f64(q) - want_q) <= err + HALF["bf16"] * np.abs(want_q)).all()
+        for b in range(B):
+            codes = [ref.decode(*(lambda c: (ref.packed(c[0], bits), c[1]))(ref.encode(f64(x)[b], bits)), bits)
+                     for x in (k, qkv[:, :, H + Hk:])]
+            for r in range(R):
+                keys = np.array([x[0] for x in kept[b]] + list(codes[0][:r + 1]))
+                vals = np.array([x[1] for x in kept[b]] + list(codes[1][:r + 1]))
+                for h in range(H):
+                    t = keys[:, h // 2] @ f64(q)[b, r, h] * D ** -0.5
+                    w = np.exp(t - t.max())
+                    want = w @ vals[:, h // 2] / w.sum()
+                    # scores within 2 (64 + 8) 2^-24 sum |q k| < 0.001; probabilities within 2^-17 more
+                    far = (np.abs(keys[:, h // 2]) @ np.abs(f64(q)[b, r, h])).max() * D ** -0.5
+                    e = (2 * 2 * 72 * 2.0 ** -24 * far + 2 * 2.0 ** -17 + 100 * 2.0 ** -24) * np.abs(vals[:, h // 2]).max()
+                    assert (np.abs(f64(out)[b, r, h] - want) <= e + HALF["bf16"] * (np.abs(want) + e)).all()
+                    assert abs(float(lse[b, r, h]) - (t.max() + math.log(w.sum()))) <= 2 * 72 * 2.0 ** -24 * far + 2.0 ** -17 + 40 * 2.0 ** -24
+            n_acc = int(rng.integers(0, R)) + 1
+            kept[b] += [(codes[0][r], codes[1][r]) for r in range(n_acc)]
+        s["lengths"] = gpu(i32([len(x) for x in kept]))
+
+
+def test_captured_steps_replay():
+    """A captured step replayed on new inputs between eager work, each replay against
+    eager calls on a copy; and two graphs whose memory is reused in between."""
+    rng = np.random.default_rng(2)
+    B, R, H, Hk, D, bits, S = 4, 2, 8, 2, 128, 4, 16
+    f = asp.rotary_frequencies(D)
+    s = step_state(rng, B, R, H, Hk, D, bits, S, 256)
+    # some context first
+    ctx = stored(rng, (B, 500, 2 * Hk, D), "bf16")
+    slots, _, s["held"], s["free"] = asp.plan_slots(s["lengths"], torch.full((B,), 500, dtype=torch.int32, device="cuda"),
+                                                    s["table"], s["held"], s["ring"], s["free"], S, width=500)
+    asp.write_cache(ctx[:, :, :Hk], ctx[:, :, Hk:], slots, s["cache"])
+    s["lengths"] = torch.full((B,), 500, dtype=torch.int32, device="cuda")
+    slots, _, s["held"], s["free"] = asp.plan_slots(s["lengths"], None, s["table"], s["held"], s["ring"], s["free"], S,
+                                                    width=4 * R)
+    x = stored(rng, (B, R, H + 2 * Hk, D), "bf16")
+    at = slots[:, :R].clone()
+    lengths = s["lengths"].clone()
+
+    def body(cache):
+        q, k = asp.rotate_heads(x[:, :, :H], x[:, :, H:H + Hk], lengths, f)
+        asp.write_cache(k, x[:, :, H + Hk:], at, cache)
+        k, v = asp.read_cache(cache, s["table"], lengths, 64, first=lengths - 60)
+        return asp.attend_cache(q, cache, s["table"], lengths, return_lse=True) + (k, v)
+    body(s["cache"])
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = body(s["cache"])
+        graphs.append((g, out))
+    mine = tuple(t.clone() for t in s["cache"])
+    for i in range(4):
+        x.copy_(stored(rng, x.shape, "bf16"))
+        at.copy_(slots[:, i * R:(i + 1) * R])
+        lengths.copy_(s["lengths"] + i * R)
+        want = [t.clone() for t in body(mine)]
+        _ = [torch.empty(1 << 20, device="cuda").fill_(float("nan")) for _ in range(4)]
+        g, out = graphs[i % 2]
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+        assert all(torch.equal(a, b) for a, b in zip(s["cache"], mine)), i
+
+
+def test_two_streams():
+    """Calls on two streams at once, each with a workspace of its own."""
+    rng = np.random.default_rng(8)
+    lengths = [3000, 100, 2000]
+    q, cache, table = attend_inputs(rng, 3, 2, 8, 2, 128, 4, 16, "bf16", lengths, garbage=False)
+    c, t, n = on_gpu(cache), gpu(table), gpu(i32(lengths))
+    p = torch.randn_like(q)
+    want = [asp.attend_cache(x, c, t, n, return_lse=True) for x in (q, p)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(20):
+        for i, x in enumerate((q, p)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(asp.attend_cache(x, c, t, n, return_lse=True))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
+
+
+def test_writes_count_as_versions():
+    x = torch.randn(2, 1, 1, 32, device="cuda")
+    cache = asp.new_cache(2, 1, 2, 32, 8)
+    before = [t._version for t in cache]
+    asp.write_cache(x, x, torch.zeros(2, 1, dtype=torch.int64, device="cuda") - 1, cache)
+    assert all(t._version > v for t, v in zip(cache, before))
+    w = x.clone().requires_grad_()
+    with pytest.raises(ValueError, match="requires a gradient"):
+        asp.rotate_heads(w, None, torch.zeros(2, dtype=torch.int32, device="cuda"), asp.rotary_frequencies(32), out=(w,))
