@@ -28,17 +28,14 @@ FLAGS = [
 def units():
     """(object name, source, defines) of every object of the library: the host
     side, the operators around the decision step and those of the cache, the
-    attention's kernels per width of codes, type of queries and kind of block size,
-    the cross-family kernels per storage type, and one object per instance of the
+    attention's kernels per width of codes and type of queries, the cross-family kernels per storage type, and one object per instance of the
     decision kernel (storage type x source of delta x variant), compiled in parallel."""
     out = [("asymspec", "asymspec.hip", []), ("step", os.path.join("step", "step.hip"), []),
            ("cache", os.path.join("cache", "cache.hip"), [])]
     for bits in (4, 8):
         for dt in (1, 0):
-            for whole in (0, 1):
-                out.insert(0, (f"attend_{bits}{dt}{whole}", os.path.join("cache", "attend.hip"),
-                               [f"-DASYMSPEC_PART_BITS={bits}", f"-DASYMSPEC_PART_DT={dt}",
-                                f"-DASYMSPEC_PART_WHOLE={whole}"]))
+            out.insert(0, (f"attend_{bits}{dt}", os.path.join("cache", "attend.hip"),
+                           [f"-DASYMSPEC_PART_BITS={bits}", f"-DASYMSPEC_PART_DT={dt}"]))
     for dt in (0, 1):
         out.append((f"xv_{dt}", "xvocab.hip", [f"-DASYMSPEC_PART_DT={dt}"]))
         for dm in (0, 1, 2):

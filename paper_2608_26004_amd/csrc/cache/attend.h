@@ -133,38 +133,82 @@ STEP_DEV void count(F&& f) {
   }
 }
 
-// 32 positions' codes as a wave's lanes load them: with j = lane % 16 and h = lane / 16,
-// of the keys of positions 16 a + j a quarter of each piece, of the values of
-// positions 4 h + i and 16 + 4 h + i a sixteenth.
+// 32 positions' codes and scales on their way through a wave's part of LDS, and as its
+// lanes then hold them: with j = lane % 16 and h = lane / 16, of the keys of positions
+// 16 a + j a quarter of each piece, of the values of positions 4 h + i and 16 + 4 h + i
+// a sixteenth.
+//
+// Memory goes to LDS past the registers, 16 bytes a lane.  Keys lie chunk by chunk (16
+// bytes of 16 positions), so that lanes j read 256 bytes in a row; values row by row,
+// position 16 a + t in row 16 a + 4 (t % 4) + t / 4, so that the four rows that are read
+// at once are neighbours.  A position's scales are one to three parts of 1, 2 or 4
+// bytes, each in a dword: [part][keys, values][position].
 template <int BITS, int D>
 struct Codes {
   typedef Pieces<D> P;
+  static constexpr int kRow = D * BITS / 8, kScales = D / kBlock;        // bytes of a position
+  static constexpr int kChunks = kRow / 16;
+  static constexpr int kPart = kScales % 4 == 0 ? 4 : kScales % 2 == 0 ? 2 : 1, kPartsOf = kScales / kPart;
+  static constexpr int kValAt = 32 * kRow, kScaleAt = 64 * kRow, kBytes = 64 * kRow + kPartsOf * 256;
   static constexpr int kKey = D * BITS / 128, kVal = BITS / 4 * P::N;     // dwords
   uint32_t key[2][kKey], val[8][kVal] = {};
-  uint8_t key_scale[2][P::N], val_scale[8][P::N];
+  uint32_t key_scale[2][P::N], val_scale[8][P::N];
 
-  STEP_DEV void load(const asymspec_cache& c, const uint32_t* key_row, const uint32_t* val_row, int j, int h) {
-    constexpr uint32_t kRow = D * BITS / 8, kScales = D / kBlock;
+  static STEP_DEV int turned(int t) { return (t & 3) * 4 + (t >> 2); }
+
+  // row: lane's, of position lane % 32.
+  static STEP_DEV void load(const asymspec_cache& c, uint32_t row, uint8_t* lds, int lane) {
 #pragma unroll
-    for (int a = 0; a < 2; ++a) {
-      const uint8_t* k = (const uint8_t*)c.keys + (uint64_t)key_row[a] * kRow;
-      const uint8_t* s = (const uint8_t*)c.key_scales + (uint64_t)key_row[a] * kScales;
-      count<P::N>([&](auto p) {
-        constexpr int w = P::width(p), from = P::base(p);
-        load_codes<w * BITS / 32>(k + from * BITS / 8 + h * (w * BITS / 32), &key[a][from * BITS / 128]);
-        key_scale[a][p] = s[(from + h * (w / 4)) / kBlock];
-      });
+    for (int n = 0; n < (32 * kChunks + 63) / 64; ++n) {
+      const int s = 64 * n + lane;
+      if (32 * kChunks % 64 != 0 && s >= 32 * kChunks) break;
+      // keys: chunk s / 16 % kChunks of position 16 (s / 16 / kChunks) + s % 16
+      const int kc = s / 16 % kChunks, kt = 16 * (s / 16 / kChunks) + s % 16;
+      const uint64_t kr = (uint32_t)__shfl(row, kt);
+      to_lds<16>((const uint8_t*)c.keys + (kr * kRow + 16 * kc), lds + 1024 * n);
+      const int vc = s % kChunks, vt = s / kChunks;
+      const uint64_t vr = (uint32_t)__shfl(row, (vt & 16) + turned(vt & 15));
+      to_lds<16>((const uint8_t*)c.values + (vr * kRow + 16 * vc), lds + kValAt + 1024 * n);
     }
+    const uint8_t* s = (const uint8_t*)(lane < 32 ? c.key_scales : c.value_scales) + (uint64_t)row * kScales;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const uint8_t* v = (const uint8_t*)c.values + (uint64_t)val_row[t] * kRow;
-      const uint8_t* s = (const uint8_t*)c.value_scales + (uint64_t)val_row[t] * kScales;
-      count<P::N>([&](auto p) {
-        constexpr int w = P::width(p), from = P::base(p);
-        load_codes<w * BITS / 128>(v + from * BITS / 8 + j * (w * BITS / 128), &val[t][p * (BITS / 4)]);
-        val_scale[t][p] = s[(from + j * (w / 16)) / kBlock];
-      });
-    }
+    for (int u = 0; u < kPartsOf; ++u) to_lds<kPart>(s + kPart * u, lds + kScaleAt + 256 * u);
+  }
+
+  template <int BYTES>
+  static STEP_DEV void to_lds(const uint8_t* from, uint8_t* to) {
+    typedef const __attribute__((address_space(1))) void* Global;
+    typedef __attribute__((address_space(3))) void* Shared;
+    if constexpr (BYTES == 16) __builtin_amdgcn_global_load_lds((Global)from, (Shared)to, 16, 0, 0);
+    else if constexpr (BYTES == 4) __builtin_amdgcn_global_load_lds((Global)from, (Shared)to, 4, 0, 0);
+    else if constexpr (BYTES == 2) __builtin_amdgcn_global_load_lds((Global)from, (Shared)to, 2, 0, 0);
+    else __builtin_amdgcn_global_load_lds((Global)from, (Shared)to, 1, 0, 0);
+  }
+
+  STEP_DEV void take(const uint8_t* lds, int j, int h) {
+    count<P::N>([&](auto p) {
+      constexpr int w = P::width(p), from = P::base(p), kOwn = w * BITS / 32, kSixteenth = w * BITS / 128;
+      const int at = from * BITS / 8 + h * kOwn, block = (from + h * (w / 4)) / kBlock;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        if constexpr (kOwn > 16) {
+#pragma unroll
+          for (int i = 0; i < kOwn / 16; ++i)
+            load_codes<16>(lds + (a * kChunks + at / 16 + i) * 256 + 16 * j, &key[a][from * BITS / 128 + 4 * i]);
+        } else {
+          load_codes<kOwn>(lds + (a * kChunks + at / 16) * 256 + 16 * j + at % 16, &key[a][from * BITS / 128]);
+        }
+        key_scale[a][p] = lds[kScaleAt + (block / kPart) * 256 + block % kPart + 4 * (16 * a + j)];
+      }
+      const int vblock = (from + j * (w / 16)) / kBlock;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int a = t / 4, i = t % 4;
+        load_codes<kSixteenth>(lds + kValAt + (16 * a + 4 * i + h) * kRow + from * BITS / 8 + j * kSixteenth,
+                               &val[t][p * (BITS / 4)]);
+        val_scale[t][p] = lds[kScaleAt + (vblock / kPart) * 256 + vblock % kPart + 4 * (32 + 16 * a + 4 * h + i)];
+      }
+    });
   }
 };
 
@@ -183,8 +227,12 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
   if (ch == 0 && A.a.lse != nullptr) A.a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
 }
 
-template <int BITS, int DT, int D, int MT, bool WHOLE>
-__global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A) {
+// Waves of an instance on a SIMD, whose registers they share: 168 each, or 256.
+template <int DT, int D, int MT>
+constexpr int attend_waves() { return DT == ASYMSPEC_BF16 && D * MT <= 128 ? 3 : 2; }
+
+template <int BITS, int DT, int D, int MT>
+__global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void attend_kernel(AttendArgs A) {
   typedef Pieces<D> P;
   typedef Codes<BITS, D> C;
   typedef typename Row<DT>::T T;
@@ -192,7 +240,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
   constexpr int kProb = DT == ASYMSPEC_BF16 ? 2 : 3;       // of a probability
   constexpr int kSteps = D / 32, kTiles = D / 16;          // matrix instructions along a head
   constexpr int kStride = D + 4;                           // of a row in LDS: 16 rows, all banks
-  __shared__ float buf[4][16][kStride];
+  // codes on their way, and at the end of a run the waves' sums
+  constexpr int kSumBytes = 4 * 16 * kStride * 4, kLds = kSumBytes > 4 * C::kBytes ? kSumBytes : 4 * C::kBytes;
+  __shared__ __align__(16) uint8_t lds[kLds];
+  float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
   __shared__ int totals[4], found[2];
 
@@ -294,48 +345,22 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
       for (int e = 0; e < kTiles; ++e) acc[m][e] = f4{0, 0, 0, 0};
     }
 
-    // Rows of the cache of 32 positions from p on: each lane looks up one position's,
-    // or, with blocks of whole sixteens, its sixteen's first.
-    auto row_of_lane = [&](int p) -> uint32_t {
-      const int position = p + (WHOLE ? lane & 16 : lane & 31);
-      uint32_t offset = (uint32_t)position;
-      const uint32_t page = A.by_size.split(offset);
-      if (position >= A.most) return kNoRow;
-      const int block = A.a.block_table[(int64_t)b * A.a.max_blocks + page];
+    // Row of the cache of the lane's position, of 32 from p on: the table's entry, and
+    // what becomes of it once it is there.
+    auto entry = [&](int p) -> int {
+      const int position = p + (lane & 31);
+      return position < A.most ? A.a.block_table[(int64_t)b * A.a.max_blocks + A.by_size.of((uint32_t)position)] : -1;
+    };
+    auto row_of = [&](int block, int p) -> uint32_t {
+      uint32_t offset = (uint32_t)(p + (lane & 31));
+      A.by_size.split(offset);
       if ((uint32_t)block >= (uint32_t)A.a.cache.blocks) return kNoRow;
       return ((uint32_t)block * (uint32_t)heads + (uint32_t)head) * (uint32_t)A.a.cache.block_size + offset;
     };
-    // (what is not there is read from row 0 and left out)
-    auto load = [&](uint32_t row, C& c, uint32_t& there) {
-      there = (uint32_t)__ballot(row != kNoRow);
-      if (row == kNoRow) row = 0;
-      uint32_t kr[2], vr[8];
-      if (WHOLE) {
-        const uint32_t r0 = __builtin_amdgcn_readlane(row, 0), r1 = __builtin_amdgcn_readlane(row, 16);
-        const uint32_t at[2] = {(there & 1u) ? r0 : 0, (there & 0x10000u) ? r1 : 0};
-        // (row 0 alone is sure to be there)
-        const uint32_t one[2] = {(there & 1u) ? 1u : 0u, (there & 0x10000u) ? 1u : 0u};
-#pragma unroll
-        for (int a = 0; a < 2; ++a) kr[a] = at[a] + one[a] * j;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) vr[t] = at[t / 4] + one[t / 4] * (4 * h + t % 4);
-      } else {
-#pragma unroll
-        for (int a = 0; a < 2; ++a) kr[a] = __shfl(row, 16 * a + j);
-#pragma unroll
-        for (int t = 0; t < 8; ++t) vr[t] = __shfl(row, 16 * (t / 4) + 4 * h + t % 4);
-      }
-      c.load(A.a.cache, kr, vr, j, h);
-    };
+    uint8_t* const own = lds + wave * C::kBytes;
 
-    const int p_first = (range.first + from) * kUnit + 32 * wave;
-    const int p_end = min(range.hi, (range.first + to) * kUnit);
-    for (int p = p_first; p < p_end; p += kUnit) {
-      if (p + 32 <= range.lo) continue;
-      const uint32_t row = row_of_lane(p);
-      C c;
-      uint32_t there;
-      load(row, c, there);
+    // What 32 positions add.
+    auto use = [&](C& c, int p, uint32_t row, uint32_t there) {
       const bool full = there == 0xFFFFFFFFu && p + 31 <= full_hi && p >= full_lo;
 
       // scores of positions 16 a + 4 h + i
@@ -402,7 +427,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
 #pragma unroll
           for (int t = 0; t < 8; ++t) {
             const int k = 16 * (t / 4) + 4 * h + t % 4;
-            const bool is = ((there >> (WHOLE ? k & 16 : k)) & 1u) && p + k <= see_hi[m] && p + k >= see_lo[m];
+            const bool is = ((there >> k) & 1u) && p + k <= see_hi[m] && p + k >= see_lo[m];
             seen |= (is ? 1u : 0u) << t;
           }
         }
@@ -451,8 +476,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
         }
         const uint32_t safe = row == kNoRow ? 0 : row;
         for (int k = 0; k < 32; ++k) {
-          if (!((there >> (WHOLE ? k & 16 : k)) & 1u)) continue;
-          const uint32_t r = WHOLE ? __shfl(safe, k & 16) + (k & 15) : __shfl(safe, k);
+          if (!((there >> k) & 1u)) continue;
+          const uint32_t r = __shfl(safe, k);
           const uint8_t* scales = (const uint8_t*)A.a.cache.value_scales + (uint64_t)r * (D / kBlock);
           const uint8_t* codes = (const uint8_t*)A.a.cache.values + (uint64_t)r * (D * BITS / 8);
 #pragma unroll
@@ -494,6 +519,34 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
             }
         });
       });
+    };
+
+    // While 32 positions are used the next ones' codes are on their way to LDS, and the
+    // table's entries of those behind them.
+    int p = (range.first + from) * kUnit + 32 * wave;
+    const int p_end = min(range.hi, (range.first + to) * kUnit);
+    if (p + 32 <= range.lo) p += kUnit;
+    if (p < p_end) {
+      uint32_t row = row_of(entry(p), p);
+      C::load(A.a.cache, row == kNoRow ? 0 : row, own, lane);
+      int next = p + kUnit < p_end ? entry(p + kUnit) : -1;
+      for (;;) {
+        C c;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        c.take(own, j, h);
+        const uint32_t there = (uint32_t)__ballot(row != kNoRow), used = row;
+        const int at = p;
+        p += kUnit;
+        if (p < p_end) {
+          // (what is read of it has arrived in registers before it is written again)
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          row = row_of(next, p);
+          C::load(A.a.cache, row == kNoRow ? 0 : row, own, lane);
+          if (p + kUnit < p_end) next = entry(p + kUnit);
+        }
+        use(c, at, used, there);
+        if (p >= p_end) break;
+      }
     }
 
     // The four waves' parts of the run, and what becomes of them.
@@ -541,6 +594,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void attend_kernel(AttendArgs A)
         }
       }
     }
+    __syncthreads();                                      // before codes go there again
   }
 }
 

@@ -1,5 +1,4 @@
-// The kernels of attend_cache for one width of codes, type of queries and kind of
-// block size.
+// The kernels of attend_cache for one width of codes and type of queries.
 
 #include <hip/hip_runtime.h>
 
@@ -10,11 +9,10 @@
 namespace asym_cache {
 
 constexpr int kBits = ASYMSPEC_PART_BITS, kType = ASYMSPEC_PART_DT;
-constexpr bool kWhole = ASYMSPEC_PART_WHOLE != 0;
 
 template <int D, int MT>
 static int attend_launch(AttendArgs& A, void* stream) {
-  const int rc = asym_step::launch(attend_kernel<kBits, kType, D, MT, kWhole>, (unsigned)A.workgroups, kAttendThreads, 0,
+  const int rc = asym_step::launch(attend_kernel<kBits, kType, D, MT>, (unsigned)A.workgroups, kAttendThreads, 0,
                                    stream, A);
   if (rc != ASYMSPEC_OK) return rc;
   const long long rows = (long long)A.a.B * A.a.cache.heads * A.rows;
@@ -32,7 +30,7 @@ static int attend_tiles(AttendArgs& A, int tiles, void* stream) {
 }
 
 template <>
-int attend_part<kBits, kType, kWhole>(AttendArgs& A, int tiles, void* stream) {
+int attend_part<kBits, kType>(AttendArgs& A, int tiles, void* stream) {
   switch (A.a.cache.dim) {
     case 64: return attend_tiles<64>(A, tiles, stream);
     case 96: return attend_tiles<96>(A, tiles, stream);

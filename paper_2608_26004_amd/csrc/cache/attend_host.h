@@ -11,7 +11,7 @@ struct AttendArgs;
 // queries and two sets of codes stay in its registers.
 constexpr int attend_most_tiles(bool bf16, int dim) { return bf16 ? (dim <= 64 ? 4 : dim <= 128 ? 2 : 1) : dim <= 64 ? 2 : 1; }
 
-template <int BITS, int DT, bool WHOLE>
+template <int BITS, int DT>
 int attend_part(AttendArgs& A, int tiles, void* stream);
 
 }  // namespace asym_cache

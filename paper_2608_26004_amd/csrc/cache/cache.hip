@@ -308,12 +308,10 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   A.c = a.scale * kLog2E;
   A.by_size = Div((uint32_t)a.cache.block_size);
   A.by_group = Div((uint32_t)A.group);
-  const bool whole = a.cache.block_size % 16 == 0, four = a.cache.bits == 4;
+  const bool four = a.cache.bits == 4;
   if (a.dtype == ASYMSPEC_BF16)
-    return four ? (whole ? attend_part<4, ASYMSPEC_BF16, true>(A, tiles, stream) : attend_part<4, ASYMSPEC_BF16, false>(A, tiles, stream))
-                : (whole ? attend_part<8, ASYMSPEC_BF16, true>(A, tiles, stream) : attend_part<8, ASYMSPEC_BF16, false>(A, tiles, stream));
-  return four ? (whole ? attend_part<4, ASYMSPEC_FP32, true>(A, tiles, stream) : attend_part<4, ASYMSPEC_FP32, false>(A, tiles, stream))
-              : (whole ? attend_part<8, ASYMSPEC_FP32, true>(A, tiles, stream) : attend_part<8, ASYMSPEC_FP32, false>(A, tiles, stream));
+    return four ? attend_part<4, ASYMSPEC_BF16>(A, tiles, stream) : attend_part<8, ASYMSPEC_BF16>(A, tiles, stream);
+  return four ? attend_part<4, ASYMSPEC_FP32>(A, tiles, stream) : attend_part<8, ASYMSPEC_FP32>(A, tiles, stream);
 }
 
 }  // extern "C"
