@@ -19,6 +19,7 @@
 #ifndef ASYMSPEC_CACHE_ATTEND_H_
 #define ASYMSPEC_CACHE_ATTEND_H_
 
+#include "attend_host.h"
 #include "format.h"
 
 namespace asym_cache {
@@ -26,6 +27,7 @@ namespace asym_cache {
 constexpr int kAttendThreads = 256;
 constexpr int kUnit = 128;                        // positions of a unit: 32 a wave
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
+constexpr uint32_t kOnes = 0x3F803F80u;           // two bf16
 constexpr float kLog2E = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -39,7 +41,8 @@ struct AttendArgs {
   int row_tiles;        // of 16 MT rows
   int most;             // positions that a table holds
   int workgroups;
-  float c;              // scale * log2 e
+  float c;              // |scale| log2 e, above 0
+  uint32_t flip;        // sign bits of a scale below 0, for the queries
   Div by_size, by_group;
 };
 
@@ -69,10 +72,6 @@ STEP_DEV float lanes_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
-STEP_DEV float lanes_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
 
 STEP_DEV uint32_t bf_pair(float a, float b) {
   const bf2 r = {(__bf16)a, (__bf16)b};
@@ -83,6 +82,18 @@ STEP_DEV float bf_high(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
 
 STEP_DEV f4 mfma(const u4& a, const u4& b, const f4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+
+// x less the low (0) or the high (1) half of a pair, in one instruction: x - 1 * half -
+// 0 * other, exact where the half is x rounded.
+template <int HALF>
+STEP_DEV float less(float x, uint32_t pair) {
+  // (in a register: as a constant of the instruction the low half's -1 was taken for the
+  // high half's)
+  uint32_t minus;
+  if (HALF == 0) asm("s_mov_b32 %0, 0x0000bf80" : "=s"(minus));
+  else asm("s_mov_b32 %0, 0xbf800000" : "=s"(minus));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2, pair), __builtin_bit_cast(bf2, minus), x, false);
 }
 
 // 8 fp32 values as N bf16 parts that add up to them, but for 2^-8N of each.
@@ -97,8 +108,8 @@ STEP_DEV void split8(const float* x, u4* parts) {
     for (int i = 0; i < 4; ++i) {
       parts[p][i] = bf_pair(rest[2 * i], rest[2 * i + 1]);
       if (p + 1 < N) {
-        rest[2 * i] -= bf_low(parts[p][i]);
-        rest[2 * i + 1] -= bf_high(parts[p][i]);
+        rest[2 * i] = less<0>(rest[2 * i], parts[p][i]);
+        rest[2 * i + 1] = less<1>(rest[2 * i + 1], parts[p][i]);
       }
     }
   }
@@ -227,12 +238,8 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
   if (ch == 0 && A.a.lse != nullptr) A.a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
 }
 
-// Waves of an instance on a SIMD, whose registers they share: 168 each, or 256.
-template <int DT, int D, int MT>
-constexpr int attend_waves() { return DT == ASYMSPEC_BF16 && D * MT <= 128 ? 3 : 2; }
-
 template <int BITS, int DT, int D, int MT>
-__global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void attend_kernel(AttendArgs A) {
+__global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
   typedef Pieces<D> P;
   typedef Codes<BITS, D> C;
   typedef typename Row<DT>::T T;
@@ -320,11 +327,13 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
         for (int s = 0; s < w / 32; ++s) {
           const T* y = x + base_ch + h * (w / 4) + 8 * s;
           if constexpr (DT == ASYMSPEC_BF16) {
-            q[m][0][base_ch / 32 + s] = asym_step::load_vec<DT>(y);
+            q[m][0][base_ch / 32 + s] = asym_step::load_vec<DT>(y) ^ A.flip;
           } else {
             float f[8];
             u4 parts[kParts];
             load8<DT>(y, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(__float_as_uint(f[e]) ^ A.flip);
             split8<kParts>(f, parts);
 #pragma unroll
             for (int k = 0; k < kParts; ++k) q[m][k][base_ch / 32 + s] = parts[k];
@@ -336,11 +345,12 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
     const int full_hi = range.len, full_lo = A.a.window > 0 ? range.len + range.fresh - A.a.window : 0;
 
     f4 acc[MT][kTiles];
-    float ref[MT], sum[MT];
+    f4 sum[MT];                                            // (each of its four the same)
+    float ref[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       ref[m] = -INFINITY;
-      sum[m] = 0.f;
+      sum[m] = f4{0, 0, 0, 0};
 #pragma unroll
       for (int e = 0; e < kTiles; ++e) acc[m][e] = f4{0, 0, 0, 0};
     }
@@ -382,23 +392,27 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
           }
         });
       }
-      uint32_t bad_key = 0, bad_val = 0;
+      // the largest of the scale bytes
+      uint32_t most_key = 0, most_val = 0;
 #pragma unroll
       for (int x = 0; x < P::N; ++x) {
 #pragma unroll
-        for (int a = 0; a < 2; ++a) bad_key |= c.key_scale[a][x] > most_scale<BITS>();
+        for (int a = 0; a < 2; ++a) most_key = max(most_key, c.key_scale[a][x]);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) bad_val |= c.val_scale[t][x] > most_scale<BITS>();
+        for (int t = 0; t < 8; ++t) most_val = max(most_val, c.val_scale[t][x]);
       }
+      bool bad_val = most_val > most_scale<BITS>();
       if (BITS == 8 && !full) {
         // (where all rows see all positions, the products spread a code that is not a
         // number as they should)
+        uint32_t any = 0;
 #pragma unroll
         for (int t = 0; t < 8; ++t)
 #pragma unroll
-          for (int x = 0; x < C::kVal; ++x) bad_val |= nan_codes(c.val[t][x]);
+          for (int x = 0; x < C::kVal; ++x) any |= nan_codes(c.val[t][x]);
+        bad_val |= any != 0;
       }
-      if (__any(bad_key)) {
+      if (__any(most_key > most_scale<BITS>())) {
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
           uint32_t of = 0;
@@ -414,28 +428,26 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
               if ((of >> (4 * h + i)) & 1u) s[m][a][i] = NAN;
         }
       }
+      if (!full) {
+        const uint32_t mine = there >> (4 * h);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const int k = 16 * (t / 4) + t % 4, at = p + 4 * h + k;
+            if (!((mine >> k) & 1u) || at > see_hi[m] || at < see_lo[m]) s[m][t / 4][t % 4] = -INFINITY;
+          }
+      }
 
       // probabilities beside the row's reference, which follows its largest score once
       // that is 2^8 above it
       u4 prob[MT][kProb];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        uint32_t seen = 0xFFu;
-        float top = -INFINITY;
-        if (!full) {
-          seen = 0;
+        float top = s[m][0][0];
 #pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            const int k = 16 * (t / 4) + 4 * h + t % 4;
-            const bool is = ((there >> k) & 1u) && p + k <= see_hi[m] && p + k >= see_lo[m];
-            seen |= (is ? 1u : 0u) << t;
-          }
-        }
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const float x = s[m][t / 4][t % 4] * A.c;
-          top = fmaxf(top, full || ((seen >> t) & 1u) ? x : -INFINITY);
-        }
+        for (int t = 1; t < 8; ++t) top = fmaxf(top, s[m][t / 4][t % 4]);
+        top *= A.c;
         if (__any(top > ref[m] + 8.f)) {
           const float next = fmaxf(ref[m], lanes_max(top));
           const float f = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ref[m] - next);
@@ -447,12 +459,11 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
         const float at = ref[m] == -INFINITY ? 0.f : ref[m];
         float w[8];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          w[t] = __builtin_amdgcn_exp2f(fmaf(s[m][t / 4][t % 4], A.c, -at));
-          if (!full) w[t] = ((seen >> t) & 1u) ? w[t] : 0.f;
-          sum[m] += w[t];
-        }
+        for (int t = 0; t < 8; ++t) w[t] = __builtin_amdgcn_exp2f(fmaf(s[m][t / 4][t % 4], A.c, -at));
         split8<kProb>(w, prob[m]);
+        // (the sum of what is multiplied with the values)
+#pragma unroll
+        for (int k = 0; k < kProb; ++k) sum[m] = mfma(u4{kOnes, kOnes, kOnes, kOnes}, prob[m][k], sum[m]);
       }
 
       float vs[8][P::N];
@@ -554,9 +565,8 @@ __global__ __launch_bounds__(kAttendThreads, (attend_waves<DT, D, MT>())) void a
     const int slot = 2 * me + (from > 0 ? 0 : 1);       // (a run that an earlier workgroup began comes first)
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      const float mine_sum = lanes_sum(sum[m]);
       __syncthreads();
-      if (h == 0) stat[wave][j] = make_float2(ref[m], mine_sum);
+      if (h == 0) stat[wave][j] = make_float2(ref[m], sum[m][0]);
       count<P::N>([&](auto pc) {
         constexpr int w = P::width(pc), base_ch = P::base(pc);
 #pragma unroll

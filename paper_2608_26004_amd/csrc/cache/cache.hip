@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "../step/launch.h"
@@ -25,6 +26,7 @@ using asym_step::Span;
 constexpr int64_t kFar = 1ll << 40;               // of a stride
 constexpr long long kMostTokens = (1ll << 31) - 16;
 constexpr int kMostHeads = 4096;
+constexpr int kUnits = 256;                       // compute units of the chip
 
 static int element(int dtype) { return dtype == ASYMSPEC_BF16 ? 2 : 4; }
 static bool typed(int dtype) { return dtype == ASYMSPEC_BF16 || dtype == ASYMSPEC_FP32; }
@@ -114,7 +116,7 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   if (runs * ((A->rows + 15) / 16) * (A->most / kUnit + 2) >= ((__int128)1 << 31)) return 0;
   if (runs * A->rows + 4 >= ((__int128)1 << 24)) return 0;
   const long long units = (long long)runs * A->row_tiles * (A->most / kUnit + 2);
-  A->workgroups = (int)std::min<long long>(units, 512);
+  A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
   const size_t slots = 2 * (size_t)A->workgroups * 16 * *tiles;
   *stats_at = ((size_t)(a.B + 1) * 4 + 15) / 16 * 16;
   *sums_at = *stats_at + slots * sizeof(float2);
@@ -305,7 +307,9 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   A.starts = (int*)workspace;
   A.stats = (float2*)((char*)workspace + stats_at);
   A.sums = (float*)((char*)workspace + sums_at);
-  A.c = a.scale * kLog2E;
+  // (a scale of 0 is far below what a score's exponent shows)
+  A.c = std::max(std::fabs(a.scale) * kLog2E, 1e-30f);
+  A.flip = std::signbit(a.scale) ? (a.dtype == ASYMSPEC_BF16 ? 0x80008000u : 0x80000000u) : 0;
   A.by_size = Div((uint32_t)a.cache.block_size);
   A.by_group = Div((uint32_t)A.group);
   const bool four = a.cache.bits == 4;
