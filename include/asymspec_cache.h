@@ -132,6 +132,7 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
 
 #define ASYMSPEC_ATTEND_MAX_REQUESTS 4096
 #define ASYMSPEC_ATTEND_MAX_ROWS 64
+#define ASYMSPEC_ATTEND_COUNTERS 524288   /* bytes at a workspace's start  */
 
 /*
  * Row r of request b stands at position p = lengths[b] + r (the lengths and
@@ -151,14 +152,17 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
  *   block_table  [B][max_blocks]; lengths [B] (negative counts as 0);
  *                new_tokens [B] (clamped to [0, R]), or NULL: R
  *   window       0 or more
- *   workspace    >= asymspec_attend_workspace_size bytes, 16-byte aligned, needs
- *                no initialisation; calls that may run at the same time (replays
- *                of captured ones among them) need distinct ones
+ *   workspace    >= asymspec_attend_workspace_size bytes, 16-byte aligned.  Its
+ *                first ASYMSPEC_ATTEND_COUNTERS bytes are zero before its first use
+ *                (of them a call uses 4 * B * heads * ceil(R * q_heads / heads / 16)
+ *                at most), and each call leaves them so for the next one, of any
+ *                shape.  Calls that may run at the same time (replays of captured
+ *                ones among them) need distinct ones
  * The outputs and the workspace overlap no other array.  dim is 64, 96, 128, 192
  * or 256; 1 <= B <= 4096, 1 <= R <= 64; q_heads is a multiple of the cache's
  * heads, at most 64 times as many; max_blocks >= 1, max_blocks * block_size below
- * 2^31 - 256, and B * heads * ceil(R * q_heads / heads / 16) * (max_blocks *
- * block_size / 128 + 2) below 2^31.
+ * 2^31 - 256, and n = B * heads * ceil(R * q_heads / heads / 16) at most
+ * 2^17, n * (max_blocks * block_size / 128 + 2) below 2^31.
  */
 typedef struct asymspec_attend {
   asymspec_cache cache;

@@ -6,8 +6,8 @@
 // whatever the requests' lengths: each takes a run of neighbouring units, of which
 // each of its four waves takes 32 positions.  A wave keeps a running reference and sum
 // for each row, so that nothing is exchanged until a run ends; there the waves' parts
-// meet in LDS, and parts of different workgroups in memory, which a second kernel
-// joins.
+// meet in LDS, and parts of different workgroups in memory, where the last one to leave
+// its part joins them (in the workgroups' order, whoever is last).
 //
 // Both products run on 16x16x32 bf16 matrix instructions.  For the scores a lane
 // decodes what it loaded, with the order of the channels permuted alike on both sides
@@ -33,9 +33,9 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
   asymspec_attend a;
-  float* sums;          // [2 workgroups][16 MT][dim]: unfinished runs
-  float2* stats;        // [2 workgroups][16 MT]: reference, sum
-  int* starts;          // [B + 1]: the requests' first units
+  uint32_t* done;       // [runs]: workgroups that have left their part; zero between calls
+  float* sums;          // [2 workgroups][16 MT][dim]: parts of runs
+  f2* stats;            // [2 workgroups][16 MT]: reference, sum
   int group;            // query heads of a head of the cache
   int rows;             // R * group
   int row_tiles;        // of 16 MT rows
@@ -238,6 +238,98 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
   if (ch == 0 && A.a.lse != nullptr) A.a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
 }
 
+// Two floats for another workgroup, which may be on another die: stored past both
+// caches.  Each place has lines of its own, which one workgroup stores and one loads in
+// a call, behind the counter, so that no cache holds them from before.  (An agent's
+// fences write back and drop a die's whole cache, which cost 100 us a call.)
+STEP_DEV void leave(float* p, float x, float y) {
+  const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
+  __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+template <class T>
+STEP_DEV T left(const T* p) { return __builtin_nontemporal_load(p); }
+
+// Joins what workgroups w0 to w1 have of a run.  A thread has eight channels of a row,
+// and with few rows a share of the parts, of which it loads six at a time.
+template <int DT, int D, int MT>
+STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, int w0, int w1, bool begins,
+                   uint8_t* lds) {
+  constexpr int kEights = D / 8, kAtOnce = 6;
+  const int rows = min(16 * MT, A.rows - row0), items = rows * kEights, parts = w1 - w0 + 1;
+  const int shares = max(1, kAttendThreads / items);
+  const int tid = threadIdx.x;
+  f4* sums = (f4*)lds;                                    // [2][threads]
+  f2* stats = (f2*)(lds + kAttendThreads * 32);
+  for (int i0 = 0; i0 < items; i0 += kAttendThreads) {
+    const int i = i0 + tid, share = shares > 1 ? i / items : 0, item = i - share * items;
+    const bool is = shares > 1 ? share < shares : i < items;
+    const int row = is ? item / kEights : 0, ch = is ? (item - row * kEights) * 8 : 0;
+    float top = -INFINITY, total = 0.f;
+    f4 o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    for (int k0 = is ? share : parts; k0 < parts; k0 += kAtOnce * shares) {
+      f4 x[kAtOnce][2];
+      f2 st[kAtOnce];
+      count<kAtOnce>([&](auto c) {
+        const int k = min(k0 + c * shares, parts - 1);
+        // (a workgroup's second place is that of a run that it begins)
+        const int64_t at = (int64_t)(2 * (w0 + k) + (k == 0 && begins ? 1 : 0)) * (16 * MT) + row;
+        st[c] = left(A.stats + at);
+        const f4* from = (const f4*)(A.sums + at * D + ch);
+        x[c][0] = left(from);
+        x[c][1] = left(from + 1);
+      });
+      float next = top;
+      count<kAtOnce>([&](auto c) {
+        if (k0 + c * shares >= parts) st[c] = f2{-INFINITY, 0.f};
+        next = fmaxf(next, st[c][0]);
+      });
+      const float at = next == -INFINITY ? 0.f : next, f = __builtin_amdgcn_exp2f(top - at);
+      top = next;
+      total *= f;
+      o[0] *= f;
+      o[1] *= f;
+      count<kAtOnce>([&](auto c) {
+        // (a part without a reference has no sums but, where its scores were no numbers, those)
+        const bool none = st[c][0] == -INFINITY && st[c][1] == 0.f;
+        const float f = none ? 0.f : st[c][0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st[c][0] - at);
+        total += st[c][1] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[0][e] = none ? o[0][e] : fmaf(x[c][0][e], f, o[0][e]);
+          o[1][e] = none ? o[1][e] : fmaf(x[c][1][e], f, o[1][e]);
+        }
+      });
+    }
+    if (shares > 1) {
+      if (is) {
+        sums[tid] = o[0];
+        sums[kAttendThreads + tid] = o[1];
+        stats[tid] = f2{top, total};
+      }
+      __syncthreads();
+      if (is && share == 0) {
+        for (int k = 1; k < shares; ++k) {
+          const f2 st = stats[k * items + item];
+          const float next = fmaxf(top, st[0]), at = next == -INFINITY ? 0.f : next;
+          const float f = __builtin_amdgcn_exp2f(top - at), g = __builtin_amdgcn_exp2f(st[0] - at);
+          top = next;
+          total = total * f + st[1] * g;
+          o[0] = o[0] * f + sums[k * items + item] * g;
+          o[1] = o[1] * f + sums[kAttendThreads + k * items + item] * g;
+        }
+      }
+    }
+    if (is && share == 0) {
+      uint32_t g = (uint32_t)(row0 + row);
+      const int r = (int)A.by_group.split(g);
+      const bool fresh = r < range.fresh;
+      for (int e = 0; e < 2; ++e)
+        finish<DT>(A, b, r, head * A.group + (int)g, D, ch + 4 * e, fresh ? top : -INFINITY, fresh ? total : 0.f,
+                   e == 0 ? o[0] : o[1]);
+    }
+  }
+}
+
 template <int BITS, int DT, int D, int MT>
 __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
   typedef Pieces<D> P;
@@ -248,11 +340,12 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
   constexpr int kSteps = D / 32, kTiles = D / 16;          // matrix instructions along a head
   constexpr int kStride = D + 4;                           // of a row in LDS: 16 rows, all banks
   // codes on their way, and at the end of a run the waves' sums
-  constexpr int kSumBytes = 4 * 16 * kStride * 4, kLds = kSumBytes > 4 * C::kBytes ? kSumBytes : 4 * C::kBytes;
+  constexpr int kJoinBytes = kAttendThreads * 40;
+  constexpr int kSumBytes = 4 * 16 * kStride * 4 > kJoinBytes ? 4 * 16 * kStride * 4 : kJoinBytes, kLds = kSumBytes > 4 * C::kBytes ? kSumBytes : 4 * C::kBytes;
   __shared__ __align__(16) uint8_t lds[kLds];
   float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
-  __shared__ int totals[4], found[2];
+  __shared__ int totals[4], found[2], is_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, h = lane >> 4;
@@ -288,12 +381,18 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
     const int b = tid * each + i;
     if (b >= A.a.B) break;
     const int n = Range(A, b).units * per_unit;
-    if (me == 0) A.starts[b] = start;
     if (u >= start && u < start + n) found[0] = b, found[1] = start;
     start += n;
-    if (me == 0 && b == A.a.B - 1) A.starts[A.a.B] = start;
   }
   __syncthreads();
+  // rows of requests without a unit
+  for (int b = me; b < A.a.B; b += (int)gridDim.x) {
+    if (Range(A, b).units > 0) continue;
+    for (int i = tid; i < A.a.R * A.a.q_heads * (D / 4); i += kAttendThreads) {
+      const int at = i / (D / 4);
+      finish<DT>(A, b, at / A.a.q_heads, at % A.a.q_heads, D, (i - at * (D / 4)) * 4, -INFINITY, 0.f, f4{0, 0, 0, 0});
+    }
+  }
   if (u >= end) return;
   int b = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
 
@@ -595,8 +694,9 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
         }
         if (!complete) {
           const int64_t at = (int64_t)slot * (16 * MT) + 16 * m + rr;
-          *(f4*)(A.sums + at * D + ch) = o;
-          if (ch == 0) A.stats[at] = make_float2(top, total);
+          leave(A.sums + at * D + ch, o[0], o[1]);
+          leave(A.sums + at * D + ch + 2, o[2], o[3]);
+          if (ch == 0) leave((float*)&A.stats[at], top, total);
         } else {
           const int r = (int)A.by_group.split(g);
           finish<DT>(A, b, r, head * A.group + (int)g, D, ch, r < range.fresh ? top : -INFINITY,
@@ -604,73 +704,23 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
         }
       }
     }
-    __syncthreads();                                      // before codes go there again
-  }
-}
-
-// Joins what several workgroups have of a run, a wave for each row; rows of requests
-// that have no unit are zero.
-template <int DT, int D, int MT>
-__global__ __launch_bounds__(kAttendThreads) void join_kernel(AttendArgs A) {
-  constexpr int kLanes = D / 4, kGroups = 64 / kLanes;      // of a row, and rows' parts at once
-  const int lane = threadIdx.x & 63;
-  const int heads = A.a.cache.heads;
-  uint32_t g = blockIdx.x * (kAttendThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b = (int)(g / (uint32_t)(heads * A.rows));
-  if (b >= A.a.B) return;
-  g -= (uint32_t)b * (uint32_t)(heads * A.rows);
-  const int head = (int)(g / (uint32_t)A.rows), row = (int)g - head * A.rows;
-  const int start = A.starts[b], all = A.starts[A.a.B];
-  const int n = (A.starts[b + 1] - start) / (heads * A.row_tiles);
-  g = (uint32_t)row;
-  const int r = (int)A.by_group.split(g), q_head = head * A.group + (int)g;
-  const int group = lane / kLanes, ch = (lane - group * kLanes) * 4;
-  const bool first = lane < kLanes;
-  if (n == 0) {
-    if (first) finish<DT>(A, b, r, q_head, D, ch, -INFINITY, 0.f, f4{0, 0, 0, 0});
-    return;
-  }
-  const int G = min(A.workgroups, all);
-  const long long u0 = start + (long long)(head * A.row_tiles + row / (16 * MT)) * n;
-  // the workgroups of units u0 and u0 + n - 1: the last w with w all / G <= u
-  const int w0 = (int)(((u0 + 1) * G - 1) / all), w1 = (int)(((u0 + n) * G - 1) / all);
-  if (w0 == w1) return;
-  // (a workgroup's second place is that of a run that it begins)
-  const bool begins = (long long)w0 * all / G <= u0;
-  auto place = [&](int w) { return (int64_t)(2 * w + (w == w0 && begins ? 1 : 0)) * (16 * MT) + row % (16 * MT); };
-  float top = -INFINITY;
-  for (int w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, A.stats[place(w)].x);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  float total = 0.f;
-  f4 o{0, 0, 0, 0};
-  if (group < kGroups) {
-    for (int w = w0 + group; w <= w1; w += kGroups) {
-      const float2 st = A.stats[place(w)];
-      const f4 x = *(const f4*)(A.sums + place(w) * D + ch);
-      const float f = st.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.x - top);
-      total += st.y * f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+    // (a part is in memory before it is counted, whichever wave stored it)
+    if (!complete) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();                                      // (codes go there again)
+    if (!complete) {
+      // the workgroups of the run's first and last unit: the last w with w all / G <= unit
+      const long long u0 = base + (long long)run * n;
+      const int w0 = (int)(((u0 + 1) * G - 1) / all), w1 = (int)(((u0 + n) * G - 1) / all);
+      const int id = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
+      if (tid == 0) {
+        is_last = __hip_atomic_fetch_add(&A.done[id], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);
+        if (is_last) __hip_atomic_store(&A.done[id], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      if (is_last) join<DT, D, MT>(A, range, b, head, row0, w0, w1, (long long)w0 * all / G <= u0, lds);
+      __syncthreads();
     }
   }
-#pragma unroll
-  for (int k = 1; k < kGroups; ++k) {
-    const int from = (lane + k * kLanes) & 63;
-    const float t = __shfl(total, from);
-    f4 x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = __shfl(o[e], from);
-    if (first) {
-      total += t;
-      // (sums of the first lanes' own, which later groups do not read)
-      o += x;
-    }
-  }
-  if (!first) return;
-  const Range range(A, b);
-  const bool is = r < range.fresh;
-  finish<DT>(A, b, r, q_head, D, ch, is ? top : -INFINITY, is ? total : 0.f, o);
 }
 
 }  // namespace asym_cache

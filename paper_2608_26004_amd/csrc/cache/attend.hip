@@ -12,11 +12,7 @@ constexpr int kBits = ASYMSPEC_PART_BITS, kType = ASYMSPEC_PART_DT;
 
 template <int D, int MT>
 static int attend_launch(AttendArgs& A, void* stream) {
-  const int rc = asym_step::launch(attend_kernel<kBits, kType, D, MT>, (unsigned)A.workgroups, kAttendThreads, 0,
-                                   stream, A);
-  if (rc != ASYMSPEC_OK) return rc;
-  const long long rows = (long long)A.a.B * A.a.cache.heads * A.rows;
-  return asym_step::launch(join_kernel<kType, D, MT>, (unsigned)((rows + 3) / 4), kAttendThreads, 0, stream, A);
+  return asym_step::launch(attend_kernel<kBits, kType, D, MT>, (unsigned)A.workgroups, kAttendThreads, 0, stream, A);
 }
 
 template <int D>

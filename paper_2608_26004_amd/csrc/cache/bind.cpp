@@ -4,7 +4,10 @@
 
 #include "../step/binding.h"
 
+#include <algorithm>
 #include <cmath>
+#include <map>
+#include <utility>
 
 #include "asymspec_cache.h"
 
@@ -161,6 +164,33 @@ PyObject* read_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Workspace of an attention on a stream: memory kept for the stream's calls, whose
+// counters each of them leaves as it found them, so that a call needs no launch to clear
+// them.  A call that is captured has memory of its own, which its replays clear: what
+// eager calls work in, a later one may replace.
+Tensor attend_workspace(size_t bytes, size_t counters, const at::Device& dev, void* stream) {
+  const auto as_bytes = at::TensorOptions().dtype(at::kByte).device(dev);
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing((hipStream_t)stream, &capture) != hipSuccess) {
+    (void)hipGetLastError();
+    check(ASYMSPEC_E_DEVICE);
+  }
+  if (capture != hipStreamCaptureStatusNone) {
+    Tensor t = at::empty({(int64_t)bytes}, as_bytes);
+    t.narrow(0, 0, (int64_t)counters).zero_();
+    return t;
+  }
+  // (never destroyed: torch's allocator may be gone before this)
+  static auto& kept = *new std::map<std::pair<int, void*>, Tensor>;
+  Tensor& t = kept[{dev.index(), stream}];
+  if (!t.defined() || (size_t)t.numel() < bytes) {
+    t = Tensor();
+    t = at::empty({(int64_t)(bytes + bytes / 4)}, as_bytes);
+    t.narrow(0, 0, ASYMSPEC_ATTEND_COUNTERS).zero_();
+  }
+  return t;
+}
+
 // q, cache, block_table, lengths, new_tokens, scale, window, return_lse, out, stream
 PyObject* attend_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 10, [&]() -> PyObject* {
@@ -201,17 +231,12 @@ PyObject* attend_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     out.is(q.scalar_type(), {B, R, H, D});
     if (with_lse) out.is(at::kFloat, {B, R, H});
     const OnDevice on(dev);
-    // a small workspace shares the outputs' allocation, a large one is given back at once
-    const bool small = bytes <= (16u << 10);
-    void* ws = out.make(dev, small ? bytes : 0);
-    Tensor own_ws;
-    if (!small) {
-      own_ws = at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(dev));
-      ws = own_ws.data_ptr();
-    }
+    out.make(dev);
+    void* const stream = stream_of(a[9]);
+    const Tensor ws = attend_workspace(bytes, 4 * std::min<size_t>((size_t)B * H * R, ASYMSPEC_ATTEND_COUNTERS / 4), dev, stream);
     s.out = out.ptr<char>("out", 0, dev);
     if (with_lse) s.lse = out.ptr<float>("lse", 1, dev);
-    check(asymspec_attend_cache(&s, ws, bytes, stream_of(a[9])));
+    check(asymspec_attend_cache(&s, ws.data_ptr(), (size_t)ws.numel(), stream));
     PyObject* r = out.result();
     if (with_lse) return r;
     PyObject* first = PyTuple_GET_ITEM(r, 0);

@@ -27,6 +27,7 @@ constexpr int64_t kFar = 1ll << 40;               // of a stride
 constexpr long long kMostTokens = (1ll << 31) - 16;
 constexpr int kMostHeads = 4096;
 constexpr int kUnits = 256;                       // compute units of the chip
+constexpr int kMostRuns = ASYMSPEC_ATTEND_COUNTERS / 4;
 
 static int element(int dtype) { return dtype == ASYMSPEC_BF16 ? 2 : 4; }
 static bool typed(int dtype) { return dtype == ASYMSPEC_BF16 || dtype == ASYMSPEC_FP32; }
@@ -114,12 +115,12 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   A->most = a.max_blocks * c.block_size;
   const __int128 runs = (__int128)a.B * c.heads;
   if (runs * ((A->rows + 15) / 16) * (A->most / kUnit + 2) >= ((__int128)1 << 31)) return 0;
-  if (runs * A->rows + 4 >= ((__int128)1 << 24)) return 0;
+  if (runs * A->row_tiles > kMostRuns) return 0;
   const long long units = (long long)runs * A->row_tiles * (A->most / kUnit + 2);
   A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
   const size_t slots = 2 * (size_t)A->workgroups * 16 * *tiles;
-  *stats_at = ((size_t)(a.B + 1) * 4 + 15) / 16 * 16;
-  *sums_at = *stats_at + slots * sizeof(float2);
+  *stats_at = kMostRuns * 4;
+  *sums_at = *stats_at + slots * sizeof(f2);
   return *sums_at + slots * c.dim * 4;
 }
 
@@ -304,8 +305,8 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
                     Span(a.lengths, b4), Span(a.new_tokens, a.new_tokens != nullptr ? b4 : 0)};
   if (asym_step::overlap(s, 3, 11)) return ASYMSPEC_E_ARG;
   if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
-  A.starts = (int*)workspace;
-  A.stats = (float2*)((char*)workspace + stats_at);
+  A.done = (uint32_t*)workspace;
+  A.stats = (f2*)((char*)workspace + stats_at);
   A.sums = (float*)((char*)workspace + sums_at);
   // (a scale of 0 is far below what a score's exponent shows)
   A.c = std::max(std::fabs(a.scale) * kLog2E, 1e-30f);
