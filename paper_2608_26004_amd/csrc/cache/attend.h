@@ -144,16 +144,20 @@ STEP_DEV void count(F&& f) {
   }
 }
 
+// Which position of sixteen is row r of a score instruction's result: a lane has rows
+// 4 h + i, i = 0 .. 3, and so positions 4 i + h, whose values' rows in LDS are neighbours
+// for the four h that read at once.
+STEP_DEV int position_of(int r) { return (r & 3) * 4 + (r >> 2); }
+
 // 32 positions' codes and scales on their way through a wave's part of LDS, and as its
-// lanes then hold them: with j = lane % 16 and h = lane / 16, of the keys of positions
-// 16 a + j a quarter of each piece, of the values of positions 4 h + i and 16 + 4 h + i
-// a sixteenth.
+// lanes then hold them: with j = lane % 16 and h = lane / 16, a quarter of each piece of
+// two keys, those of row j of either sixteen, and a sixteenth of eight values, those of
+// rows 4 h + i.
 //
-// Memory goes to LDS past the registers, 16 bytes a lane.  Keys lie chunk by chunk (16
-// bytes of 16 positions), so that lanes j read 256 bytes in a row; values row by row,
-// position 16 a + t in row 16 a + 4 (t % 4) + t / 4, so that the four rows that are read
-// at once are neighbours.  A position's scales are one to three parts of 1, 2 or 4
-// bytes, each in a dword: [part][keys, values][position].
+// Memory goes to LDS past the registers, 16 bytes a lane and rows in their order.  Where
+// a row is 2^k chunks of 16 bytes, a key's chunks are exchanged so that the chunks that
+// 16 lanes read at once lie in different banks.  A position's scales are one to three
+// parts of 1, 2 or 4 bytes, each in a dword: [part][keys, values][position].
 template <int BITS, int D>
 struct Codes {
   typedef Pieces<D> P;
@@ -165,21 +169,21 @@ struct Codes {
   uint32_t key[2][kKey], val[8][kVal] = {};
   uint32_t key_scale[2][P::N], val_scale[8][P::N];
 
-  static STEP_DEV int turned(int t) { return (t & 3) * 4 + (t >> 2); }
+  // Where a chunk of a position's key lies in its row.
+  static STEP_DEV int chunk_at(int t, int chunk) {
+    constexpr bool kExchanged = (kChunks & (kChunks - 1)) == 0;
+    return kExchanged ? chunk ^ ((t & 15) * kChunks / 16) : chunk;
+  }
 
   // row: lane's, of position lane % 32.
   static STEP_DEV void load(const asymspec_cache& c, uint32_t row, uint8_t* lds, int lane) {
 #pragma unroll
     for (int n = 0; n < (32 * kChunks + 63) / 64; ++n) {
-      const int s = 64 * n + lane;
+      const int s = 64 * n + lane, t = s / kChunks, at = s % kChunks;
       if (32 * kChunks % 64 != 0 && s >= 32 * kChunks) break;
-      // keys: chunk s / 16 % kChunks of position 16 (s / 16 / kChunks) + s % 16
-      const int kc = s / 16 % kChunks, kt = 16 * (s / 16 / kChunks) + s % 16;
-      const uint64_t kr = (uint32_t)__shfl(row, kt);
-      to_lds<16>((const uint8_t*)c.keys + (kr * kRow + 16 * kc), lds + 1024 * n);
-      const int vc = s % kChunks, vt = s / kChunks;
-      const uint64_t vr = (uint32_t)__shfl(row, (vt & 16) + turned(vt & 15));
-      to_lds<16>((const uint8_t*)c.values + (vr * kRow + 16 * vc), lds + kValAt + 1024 * n);
+      const uint64_t r = (uint32_t)__shfl(row, t);
+      to_lds<16>((const uint8_t*)c.keys + (r * kRow + 16 * chunk_at(t, at)), lds + 1024 * n);
+      to_lds<16>((const uint8_t*)c.values + (r * kRow + 16 * at), lds + kValAt + 1024 * n);
     }
     const uint8_t* s = (const uint8_t*)(lane < 32 ? c.key_scales : c.value_scales) + (uint64_t)row * kScales;
 #pragma unroll
@@ -197,19 +201,21 @@ struct Codes {
   }
 
   STEP_DEV void take(const uint8_t* lds, int j, int h) {
+    const int t = position_of(j);
     count<P::N>([&](auto p) {
       constexpr int w = P::width(p), from = P::base(p), kOwn = w * BITS / 32, kSixteenth = w * BITS / 128;
       const int at = from * BITS / 8 + h * kOwn, block = (from + h * (w / 4)) / kBlock;
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
+        const uint8_t* row = lds + (16 * a + t) * kRow;
         if constexpr (kOwn > 16) {
 #pragma unroll
           for (int i = 0; i < kOwn / 16; ++i)
-            load_codes<16>(lds + (a * kChunks + at / 16 + i) * 256 + 16 * j, &key[a][from * BITS / 128 + 4 * i]);
+            load_codes<16>(row + 16 * chunk_at(t, at / 16 + i), &key[a][from * BITS / 128 + 4 * i]);
         } else {
-          load_codes<kOwn>(lds + (a * kChunks + at / 16) * 256 + 16 * j + at % 16, &key[a][from * BITS / 128]);
+          load_codes<kOwn>(row + 16 * chunk_at(t, at / 16) + at % 16, &key[a][from * BITS / 128]);
         }
-        key_scale[a][p] = lds[kScaleAt + (block / kPart) * 256 + block % kPart + 4 * (16 * a + j)];
+        key_scale[a][p] = lds[kScaleAt + (block / kPart) * 256 + block % kPart + 4 * (16 * a + t)];
       }
       const int vblock = (from + j * (w / 16)) / kBlock;
 #pragma unroll
@@ -217,7 +223,7 @@ struct Codes {
         const int a = t / 4, i = t % 4;
         load_codes<kSixteenth>(lds + kValAt + (16 * a + 4 * i + h) * kRow + from * BITS / 8 + j * kSixteenth,
                                &val[t][p * (BITS / 4)]);
-        val_scale[t][p] = lds[kScaleAt + (vblock / kPart) * 256 + vblock % kPart + 4 * (32 + 16 * a + 4 * h + i)];
+        val_scale[t][p] = lds[kScaleAt + (vblock / kPart) * 256 + vblock % kPart + 4 * (32 + 16 * a + 4 * i + h)];
       }
     });
   }
@@ -472,7 +478,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
     auto use = [&](C& c, int p, uint32_t row, uint32_t there) {
       const bool full = there == 0xFFFFFFFFu && p + 31 <= full_hi && p >= full_lo;
 
-      // scores of positions 16 a + 4 h + i
+      // scores of positions 16 a + 4 i + h
       f4 s[MT][2];
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
@@ -528,12 +534,12 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
         }
       }
       if (!full) {
-        const uint32_t mine = there >> (4 * h);
+        const uint32_t mine = there >> h;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int t = 0; t < 8; ++t) {
-            const int k = 16 * (t / 4) + t % 4, at = p + 4 * h + k;
+            const int k = 16 * (t / 4) + 4 * (t % 4), at = p + h + k;
             if (!((mine >> k) & 1u) || at > see_hi[m] || at < see_lo[m]) s[m][t / 4][t % 4] = -INFINITY;
           }
       }
