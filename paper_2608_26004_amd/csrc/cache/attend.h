@@ -58,9 +58,10 @@ template <int D> struct Pieces {
 // [lo, hi), and its number of rows.
 struct Range {
   int len, fresh, lo, hi, first, units;
-  STEP_DEV Range(const AttendArgs& A, int b) {
-    len = min(max(A.a.lengths[b], 0), 0x7FFFFF00);
-    fresh = A.a.new_tokens != nullptr ? min(max(A.a.new_tokens[b], 0), A.a.R) : A.a.R;
+  STEP_DEV Range(const AttendArgs& A, int b)
+      : Range(A, min(max(A.a.lengths[b], 0), 0x7FFFFF00),
+              A.a.new_tokens != nullptr ? min(max(A.a.new_tokens[b], 0), A.a.R) : A.a.R) {}
+  STEP_DEV Range(const AttendArgs& A, int len_, int fresh_) : len(len_), fresh(fresh_) {
     hi = min(len + fresh, A.most);
     lo = A.a.window > 0 ? max(0, len - A.a.window + 1) : 0;
     first = lo / kUnit;
@@ -237,9 +238,10 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
   typedef typename Row<DT>::T T;
   const int64_t at = ((int64_t)b * A.a.R + r) * A.a.q_heads + q_head;
   const bool none = sum == 0.f;
+  const float over = 1.f / sum;
   float y[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : o[e] / sum;
+  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : o[e] * over;
   T* out = (T*)A.a.out + at * dim + ch;
   if constexpr (DT == ASYMSPEC_BF16) *(u2*)out = u2{bf_pair(y[0], y[1]), bf_pair(y[2], y[3])};
   else *(f4*)out = f4{y[0], y[1], y[2], y[3]};
@@ -258,11 +260,12 @@ template <class T>
 STEP_DEV T left(const T* p) { return __builtin_nontemporal_load(p); }
 
 // Joins what workgroups w0 to w1 have of a run.  A thread has eight channels of a row,
-// and with few rows a share of the parts, of which it loads six at a time.
+// and with few rows a share of the parts, of which it loads four at a time (more at once, or fewer,
+// take as long: what counts is that this code, which runs once, is short).
 template <int DT, int D, int MT>
 STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, int w0, int w1, bool begins,
                    uint8_t* lds) {
-  constexpr int kEights = D / 8, kAtOnce = 6;
+  constexpr int kEights = D / 8, kAtOnce = 4;
   const int rows = min(16 * MT, A.rows - row0), items = rows * kEights, parts = w1 - w0 + 1;
   const int shares = max(1, kAttendThreads / items);
   const int tid = threadIdx.x;
@@ -353,7 +356,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
   __shared__ __align__(16) uint8_t lds[kLds];
   float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
-  __shared__ int totals[4], found[2], is_last;
+  __shared__ int totals[4], found[4], is_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, h = lane >> 4;
@@ -361,11 +364,10 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
 
   // The requests' first units in the list, and the request of this workgroup's first one.
   const int each = (A.a.B + kAttendThreads - 1) / kAttendThreads;
-  int mine = 0;
-  for (int i = 0; i < each; ++i) {
-    const int b = tid * each + i;
-    if (b < A.a.B) mine += Range(A, b).units * per_unit;
-  }
+  const Range lane_first(A, min(tid * each, A.a.B - 1));    // (a thread's only one, up to 256 requests)
+  int mine = tid * each < A.a.B ? lane_first.units * per_unit : 0;
+  for (int i = 1; i < each; ++i)
+    if (tid * each + i < A.a.B) mine += Range(A, tid * each + i).units * per_unit;
   int upto = mine;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -375,9 +377,11 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
   if (lane == 63) totals[wave] = upto;
   __syncthreads();
   int start = upto - mine, all = 0;
+#pragma unroll
   for (int w = 0; w < 4; ++w) {
-    if (w < wave) start += totals[w];
-    all += totals[w];
+    const int t = totals[w];
+    if (w < wave) start += t;
+    all += t;
   }
   const int G = min(A.workgroups, all), me = blockIdx.x;
   int u = 0, end = 0;
@@ -385,31 +389,24 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
     u = (int)((long long)me * all / G);
     end = (int)((long long)(me + 1) * all / G);
   }
-  for (int i = 0; i < each; ++i) {
-    const int b = tid * each + i;
-    if (b >= A.a.B) break;
-    const int n = Range(A, b).units * per_unit;
-    if (u >= start && u < start + n) found[0] = b, found[1] = start;
-    start += n;
+  if (u >= start && u < start + mine) {
+    Range r = lane_first;
+    int b = tid * each;
+    while (u >= start + r.units * per_unit) {
+      start += r.units * per_unit;
+      r = Range(A, ++b);
+    }
+    found[0] = b, found[1] = start, found[2] = r.len, found[3] = r.fresh;
   }
   __syncthreads();
-  // rows of requests without a unit
-  for (int b = me; b < A.a.B; b += (int)gridDim.x) {
-    if (Range(A, b).units > 0) continue;
-    for (int i = tid; i < A.a.R * A.a.q_heads * (D / 4); i += kAttendThreads) {
-      const int at = i / (D / 4);
-      finish<DT>(A, b, at / A.a.q_heads, at % A.a.q_heads, D, (i - at * (D / 4)) * 4, -INFINITY, 0.f, f4{0, 0, 0, 0});
-    }
-  }
-  if (u >= end) return;
   int b = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
+  Range range(A, __builtin_amdgcn_readfirstlane(found[2]), __builtin_amdgcn_readfirstlane(found[3]));
 
   while (u < end) {
-    const Range range(A, b);
     const int n = range.units;
     if (u >= base + n * per_unit) {
       base += n * per_unit;
-      ++b;
+      range = Range(A, ++b);
       continue;
     }
     const int run = (u - base) / n, from = (u - base) - run * n, to = min(n, from + (end - u));
@@ -651,6 +648,8 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
       for (;;) {
         C c;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // (a wave whose codes are there asks for the next ones ahead of the others' arithmetic)
+        __builtin_amdgcn_s_setprio(3);
         c.take(own, j, h);
         const uint32_t there = (uint32_t)__ballot(row != kNoRow), used = row;
         const int at = p;
@@ -662,6 +661,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
           C::load(A.a.cache, row == kNoRow ? 0 : row, own, lane);
           if (p + kUnit < p_end) next = entry(p + kUnit);
         }
+        __builtin_amdgcn_s_setprio(0);
         use(c, at, used, there);
         if (p >= p_end) break;
       }
@@ -727,6 +727,15 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
       __syncthreads();
       if (is_last) join<DT, D, MT>(A, range, b, head, row0, w0, w1, (long long)w0 * all / G <= u0, lds);
       __syncthreads();
+    }
+  }
+
+  // rows of requests without a unit
+  for (int b = me; b < A.a.B; b += (int)gridDim.x) {
+    if (Range(A, b).units > 0) continue;
+    for (int i = tid; i < A.a.R * A.a.q_heads * (D / 4); i += kAttendThreads) {
+      const int at = i / (D / 4);
+      finish<DT>(A, b, at / A.a.q_heads, at % A.a.q_heads, D, (i - at * (D / 4)) * 4, -INFINITY, 0.f, f4{0, 0, 0, 0});
     }
   }
 }
