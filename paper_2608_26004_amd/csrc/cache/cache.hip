@@ -87,15 +87,21 @@ static int rotate_launch(const RotateArgs& A, unsigned grid, size_t lds, bool ve
   return launch(kernel, grid, kRotateThreads, lds, stream, a);
 }
 
-// How a tile's items are shared.
-static void move_parts(MoveArgs& M) {
+// How tokens (of `requests`, each on its own) and heads are shared: as many tokens as a
+// workgroup has lanes for, and as many heads as leave four workgroups to a unit.
+// Returns the workgroups, or -1 where they are too many.
+static long long move_parts(MoveArgs& M, int requests) {
   const uint32_t lanes = (uint32_t)M.c.dim / 8;
-  M.items = 2u * (uint32_t)M.c.heads * kMoveTile * lanes;
-  M.groups = (M.items + kMoveThreads - 1) / kMoveThreads;
+  M.tile = kMoveThreads / lanes;
+  const long long per = ((long long)M.tokens + M.tile - 1) / M.tile, tiles = per * requests;
+  const int groups = (int)std::min<long long>(M.c.heads, std::max<long long>(1, 4 * kUnits / tiles));
+  M.heads = (uint32_t)((M.c.heads + groups - 1) / groups);
+  const uint32_t used = ((uint32_t)M.c.heads + M.heads - 1) / M.heads;
   M.by_lanes = Div(lanes);
-  M.by_heads = Div((uint32_t)M.c.heads);
   M.by_size = Div((uint32_t)M.c.block_size);
-  M.by_groups = Div(M.groups);
+  M.by_groups = Div(used);
+  M.by_tiles = Div((uint32_t)per);
+  return tiles < (1ll << 24) && fits(tiles * used, kMoveThreads) ? tiles * used : -1;
 }
 
 // Row tiles of 16 rows, and the workspace of an attention; 0 for invalid sizes.
@@ -224,11 +230,9 @@ int asymspec_write_cache(const asymspec_cache* cache, const asymspec_heads* k, c
   if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
   M.slots = slots;
   M.tokens = (uint32_t)((long long)B * R);
-  M.tiles = (M.tokens + kMoveTile - 1) / kMoveTile;
   M.by_R = Div((uint32_t)R);
-  move_parts(M);
-  const long long grid = (long long)M.tiles * M.groups;
-  if (!fits(grid, kMoveThreads)) return ASYMSPEC_E_ARG;
+  const long long grid = move_parts(M, 1);
+  if (grid < 0) return ASYMSPEC_E_ARG;
   auto* kernel = dtype == ASYMSPEC_BF16
                      ? (M.c.bits == 4 ? write_kernel<ASYMSPEC_BF16, 4> : write_kernel<ASYMSPEC_BF16, 8>)
                      : (M.c.bits == 4 ? write_kernel<ASYMSPEC_FP32, 4> : write_kernel<ASYMSPEC_FP32, 8>);
@@ -259,11 +263,8 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
   M.k.at = k;
   M.v.at = v;
   M.tokens = (uint32_t)width;
-  M.tiles = (uint32_t)((width + kMoveTile - 1ll) / kMoveTile);
-  M.by_tiles = Div(M.tiles);
-  move_parts(M);
-  const __int128 grid = (__int128)B * M.tiles * M.groups;
-  if (grid >= ((__int128)1 << 24)) return ASYMSPEC_E_ARG;
+  const long long grid = move_parts(M, B);
+  if (grid < 0) return ASYMSPEC_E_ARG;
   if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
   auto* kernel = dtype == ASYMSPEC_BF16 ? (M.c.bits == 4 ? read_kernel<ASYMSPEC_BF16, 4> : read_kernel<ASYMSPEC_BF16, 8>)
                                         : (M.c.bits == 4 ? read_kernel<ASYMSPEC_FP32, 4> : read_kernel<ASYMSPEC_FP32, 8>);
