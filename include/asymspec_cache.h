@@ -107,7 +107,7 @@ int asymspec_rotate_heads(const asymspec_rotate* rotate, void* stream);
  *   slots   [B][R]; out of [0, blocks * block_size): the token is left out.
  *           The slots of a call are distinct (one given twice holds a mix)
  * Nothing else in the cache changes.  B, R >= 1; heads at most 4096;
- * ceil(B * R / floor(2048 / dim)) below 2^24.
+ * ceil(B * R / floor(2048 / dim)) * heads below 2^24.
  */
 int asymspec_write_cache(const asymspec_cache* cache, const asymspec_heads* k, const asymspec_heads* v, int dtype,
                          const int64_t* slots, int B, int R, void* stream);
@@ -122,8 +122,8 @@ int asymspec_write_cache(const asymspec_cache* cache, const asymspec_heads* k, c
  * [0, blocks) gives zeros.
  *   first   [B] or NULL: 0
  *   k, v    out, contiguous, 16-byte aligned; either may be NULL
- * B, width, max_blocks >= 1; heads at most 4096; B * ceil(width / floor(2048 / dim))
- * below 2^24.
+ * B, width, max_blocks >= 1; heads at most 4096; B * ceil(width /
+ * floor(2048 / dim)) * heads below 2^24.
  */
 int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table, int max_blocks, const int32_t* lengths,
                         const int32_t* first, int dtype, int B, int width, void* k, void* v, void* stream);

@@ -88,20 +88,19 @@ static int rotate_launch(const RotateArgs& A, unsigned grid, size_t lds, bool ve
 }
 
 // How tokens (of `requests`, each on its own) and heads are shared: as many tokens as a
-// workgroup has lanes for, and as many heads as leave four workgroups to a unit.
-// Returns the workgroups, or -1 where they are too many.
+// workgroup has lanes for, and two heads, or one where that leaves fewer than four
+// workgroups to a unit.  Returns the workgroups, or -1 where they are too many.
 static long long move_parts(MoveArgs& M, int requests) {
-  const uint32_t lanes = (uint32_t)M.c.dim / 8;
+  const uint32_t lanes = (uint32_t)M.c.dim / 8, heads = (uint32_t)M.c.heads;
   M.tile = kMoveThreads / lanes;
   const long long per = ((long long)M.tokens + M.tile - 1) / M.tile, tiles = per * requests;
-  const int groups = (int)std::min<long long>(M.c.heads, std::max<long long>(1, 4 * kUnits / tiles));
-  M.heads = (uint32_t)((M.c.heads + groups - 1) / groups);
-  const uint32_t used = ((uint32_t)M.c.heads + M.heads - 1) / M.heads;
+  M.heads = tiles * heads >= 4ll * kUnits * kMoveHeads ? kMoveHeads : 1;
+  const uint32_t groups = (heads + M.heads - 1) / M.heads;
   M.by_lanes = Div(lanes);
   M.by_size = Div((uint32_t)M.c.block_size);
-  M.by_groups = Div(used);
+  M.by_groups = Div(groups);
   M.by_tiles = Div((uint32_t)per);
-  return tiles < (1ll << 24) && fits(tiles * used, kMoveThreads) ? tiles * used : -1;
+  return tiles < (1ll << 24) && tiles * heads < (1ll << 24) ? tiles * groups : -1;
 }
 
 // Row tiles of 16 rows, and the workspace of an attention; 0 for invalid sizes.

@@ -1,9 +1,13 @@
-// write_cache and read_cache: a lane has 8 channels of a token, and all heads of a group
-// of theirs, keys and values, one after the other.  A token's place is looked up once;
-// what a head adds is a constant.  Lanes run along a head's channels and then along
-// tokens that are neighbours, in a block of the cache too, so that both sides move whole
-// lines.  (With a head a lane the index arithmetic took longer than the memory: 65536
-// tokens of 8 heads of 128 channels to 4 bits 95 us, and back 86.)
+// write_cache and read_cache: a lane has 8 channels of a token, keys and values of two
+// heads, whose loads are under way together.  A token's place is looked up once; what a
+// head adds is a constant.  Lanes run along a head's channels and then along tokens that
+// are neighbours, in a block of the cache too, so that both sides move whole lines.
+//
+// Bound by memory: 65536 tokens of 8 heads of 128 channels from bf16 to 4 bits and back
+// take 119 us for 679 MB, 16 x 8192 positions back 124 for 644 MB (5.2 TB/s and more; a
+// copy reaches 5.1).  With one head's key or value a lane the index arithmetic took
+// longer than that (176, 181 us); with one head a lane they take 139 and 133, with all
+// eight 132 and 134; with loads that leave lines in the caches 138 and 125.
 
 #ifndef ASYMSPEC_CACHE_MOVE_H_
 #define ASYMSPEC_CACHE_MOVE_H_
@@ -13,7 +17,7 @@
 namespace asym_cache {
 
 constexpr int kMoveThreads = 256;
-constexpr int kMoveAtOnce = 4;
+constexpr int kMoveHeads = 2;         // of a lane
 
 struct MoveArgs {
   asymspec_cache c;
@@ -22,7 +26,7 @@ struct MoveArgs {
   const int32_t *table, *lengths, *first;   // read
   uint32_t tokens;                 // write: B * R; read: width
   uint32_t tile;                   // tokens of a workgroup
-  uint32_t heads;                  // of a workgroup
+  uint32_t heads;                  // of a workgroup: at most kMoveHeads
   int max_blocks;
   Div by_lanes, by_size, by_R, by_groups, by_tiles;
 };
@@ -33,20 +37,16 @@ STEP_DEV uint32_t quad_max(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));
 }
 
-// Calls load(i, which, head, slot of kMoveAtOnce) and then use of the same for the group's
-// heads, kMoveAtOnce at a time.
+// Calls load(i, which, head) for the keys (which = 0) and values of each of the heads,
+// and then use of the same.
 template <class Load, class Use>
 STEP_DEV void each_head(uint32_t from, uint32_t to, Load&& load, Use&& use) {
-  static_assert(kMoveAtOnce == 4);
-  uint32_t h = from;
-  for (; h + 1 < to; h += 2) {
-    load(0, 0, h), load(1, 1, h), load(2, 0, h + 1), load(3, 1, h + 1);
-    use(0, 0, h), use(1, 1, h), use(2, 0, h + 1), use(3, 1, h + 1);
-  }
-  if (h < to) {
-    load(0, 0, h), load(1, 1, h);
-    use(0, 0, h), use(1, 1, h);
-  }
+  static_assert(kMoveHeads == 2);
+  const bool two = from + 1 < to;
+  load(0, 0, from), load(1, 1, from);
+  if (two) load(2, 0, from + 1), load(3, 1, from + 1);
+  use(0, 0, from), use(1, 1, from);
+  if (two) use(2, 0, from + 1), use(3, 1, from + 1);
 }
 
 template <int DT, int BITS>
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kMoveThreads) void write_kernel(MoveArgs A) {
   const T* const v = (const T*)A.v.at + (b * A.v.request + row * A.v.row) + c8 * 8;
   const uint32_t size = (uint32_t)A.c.block_size, bytes = (uint32_t)(A.c.dim * BITS / 8), scales = (uint32_t)(A.c.dim / kBlock);
   const uint64_t first = (uint64_t)block * (uint32_t)A.c.heads * size + offset;
-  float f[kMoveAtOnce][8];
+  float f[2 * kMoveHeads][8];
   each_head(
       group * A.heads, min((group + 1) * A.heads, (uint32_t)A.c.heads),
       [&](int i, int which, uint32_t head) { load8<DT>(which ? v + head * A.v.head : k + head * A.k.head, f[i]); },
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kMoveThreads) void read_kernel(MoveArgs A) {
   const bool there = (uint32_t)block < (uint32_t)A.c.blocks;
   const uint64_t first = there ? (uint64_t)block * (uint32_t)A.c.heads * size + offset : 0;
   const int64_t to = ((int64_t)b * A.tokens + token) * (uint32_t)A.c.heads * A.c.dim + c8 * 8;
-  uint32_t codes[kMoveAtOnce][2], byte[kMoveAtOnce];
+  uint32_t codes[2 * kMoveHeads][2], byte[2 * kMoveHeads];
   each_head(
       group * A.heads, min((group + 1) * A.heads, (uint32_t)A.c.heads),
       [&](int i, int which, uint32_t head) {
@@ -114,9 +114,9 @@ __global__ __launch_bounds__(kMoveThreads) void read_kernel(MoveArgs A) {
         const uint64_t at = first + (uint64_t)head * size;
         const uint8_t* data = (const uint8_t*)(which ? A.c.values : A.c.keys) + at * bytes + c8 * BITS;
         if (BITS == 4) {
-          codes[i][0] = *(const uint32_t*)data;
+          codes[i][0] = __builtin_nontemporal_load((const uint32_t*)data);
         } else {
-          const u2 x = *(const u2*)data;
+          const u2 x = __builtin_nontemporal_load((const u2*)data);
           codes[i][0] = x[0], codes[i][1] = x[1];
         }
         byte[i] = ((const uint8_t*)(which ? A.c.value_scales : A.c.key_scales))[at * scales + c8 / 4];
