@@ -79,12 +79,22 @@ static bool same(const asymspec_heads& a, const asymspec_heads& b) {
 }
 static bool meet(const Span& a, const Span& b) { return a.from < b.to && b.from < a.to; }
 
-template <int DT>
-static int rotate_launch(const RotateArgs& A, unsigned grid, size_t lds, bool vec, void* stream) {
-  RotateArgs a = A;
-  auto* kernel = A.r.interleaved ? (vec ? rotate_kernel<DT, true, true> : rotate_kernel<DT, true, false>)
-                                 : (vec ? rotate_kernel<DT, false, true> : rotate_kernel<DT, false, false>);
-  return launch(kernel, grid, kRotateThreads, lds, stream, a);
+// Inputs from here on pass the caches by: smaller ones are often still there from the
+// kernel that wrote them.  (Rotations of 29 MB 11.4 us with the caches, 13.6 past them;
+// of 115 MB 38.5 and 38.2; of 229 MB 83 and 70.  Writes of 59 MB in 4 bits 14.8 and 16.1;
+// of 118 MB 30.2 and 27.7.)
+constexpr int64_t kOnce = 96 << 20;
+
+template <int DT, bool INTER>
+static int rotate_launch(RotateArgs& A, unsigned grid, size_t lds, bool vec, bool once, void* stream) {
+  auto* kernel = !vec ? rotate_kernel<DT, INTER, false, false>
+                      : once ? rotate_kernel<DT, INTER, true, true> : rotate_kernel<DT, INTER, true, false>;
+  return launch(kernel, grid, kRotateThreads, lds, stream, A);
+}
+
+template <int DT, int BITS>
+static int write_launch(MoveArgs& M, unsigned grid, bool once, void* stream) {
+  return launch(once ? write_kernel<DT, BITS, true> : write_kernel<DT, BITS, false>, grid, kMoveThreads, 0, stream, M);
 }
 
 // How tokens (of `requests`, each on its own) and heads are shared: as many tokens as a
@@ -195,8 +205,11 @@ int asymspec_rotate_heads(const asymspec_rotate* rotate, void* stream) {
   const bool copies = !same(r.q, r.q_out) || (r.k_heads > 0 && !same(r.k, r.k_out));
   A.tail = copies ? (uint32_t)(vec ? rest / ve : rest) : 0;
   A.pieces = (uint32_t)(vec ? (r.interleaved ? 2 * r.n : r.n) / ve : r.n) + A.tail;
+  // A workgroup has one token, or as many as give a quarter of its threads an angle, as
+  // long as a unit has four workgroups.  (16384 tokens of 40 heads of 128 channels: one
+  // token 58 us, two 61, four 64.)
   A.T = 1;
-  while (A.T < kRotateMostTokens && A.T * r.n < kRotateThreads && A.tokens > 4u * (uint32_t)cus * (uint32_t)A.T) A.T *= 2;
+  while (A.T < kRotateMostTokens && A.T * r.n < kRotateThreads / 4 && A.tokens > 4u * (uint32_t)cus * (uint32_t)A.T) A.T *= 2;
   A.by_n = Div((uint32_t)r.n);
   A.by_R = Div((uint32_t)r.R);
   A.by_pieces = Div(A.pieces);
@@ -204,8 +217,12 @@ int asymspec_rotate_heads(const asymspec_rotate* rotate, void* stream) {
   const long long grid = (A.tokens + (long long)A.T - 1) / A.T;
   if (!fits(grid, kRotateThreads)) return ASYMSPEC_E_ARG;
   const size_t lds = (size_t)A.T * r.n * sizeof(float2);
-  return r.dtype == ASYMSPEC_BF16 ? rotate_launch<ASYMSPEC_BF16>(A, (unsigned)grid, lds, vec, stream)
-                                  : rotate_launch<ASYMSPEC_FP32>(A, (unsigned)grid, lds, vec, stream);
+  const bool once = (int64_t)A.tokens * (r.q_heads + r.k_heads) * r.dim * el >= kOnce;
+  if (r.dtype == ASYMSPEC_BF16)
+    return r.interleaved ? rotate_launch<ASYMSPEC_BF16, true>(A, (unsigned)grid, lds, vec, once, stream)
+                         : rotate_launch<ASYMSPEC_BF16, false>(A, (unsigned)grid, lds, vec, once, stream);
+  return r.interleaved ? rotate_launch<ASYMSPEC_FP32, true>(A, (unsigned)grid, lds, vec, once, stream)
+                       : rotate_launch<ASYMSPEC_FP32, false>(A, (unsigned)grid, lds, vec, once, stream);
 }
 
 int asymspec_write_cache(const asymspec_cache* cache, const asymspec_heads* k, const asymspec_heads* v, int dtype,
@@ -232,10 +249,12 @@ int asymspec_write_cache(const asymspec_cache* cache, const asymspec_heads* k, c
   M.by_R = Div((uint32_t)R);
   const long long grid = move_parts(M, 1);
   if (grid < 0) return ASYMSPEC_E_ARG;
-  auto* kernel = dtype == ASYMSPEC_BF16
-                     ? (M.c.bits == 4 ? write_kernel<ASYMSPEC_BF16, 4> : write_kernel<ASYMSPEC_BF16, 8>)
-                     : (M.c.bits == 4 ? write_kernel<ASYMSPEC_FP32, 4> : write_kernel<ASYMSPEC_FP32, 8>);
-  return launch(kernel, (unsigned)grid, kMoveThreads, 0, stream, M);
+  const bool four = M.c.bits == 4, once = 2ll * M.tokens * M.c.heads * M.c.dim * element(dtype) >= kOnce;
+  if (dtype == ASYMSPEC_BF16)
+    return four ? write_launch<ASYMSPEC_BF16, 4>(M, (unsigned)grid, once, stream)
+                : write_launch<ASYMSPEC_BF16, 8>(M, (unsigned)grid, once, stream);
+  return four ? write_launch<ASYMSPEC_FP32, 4>(M, (unsigned)grid, once, stream)
+              : write_launch<ASYMSPEC_FP32, 8>(M, (unsigned)grid, once, stream);
 }
 
 int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table, int max_blocks, const int32_t* lengths,

@@ -106,21 +106,22 @@ STEP_DEV u4 decode8(const uint32_t* codes, float scale) {
               decode2<8, 1>(codes[1], scale)};
 }
 
-// 16 bytes of a row that are read once, wherever they begin: the caches keep no line.
-template <int DT>
-STEP_DEV u4 load_once(const typename Row<DT>::T* p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const typename Row<DT>::U*>(p));
+// 16 bytes of a row, wherever they begin.  ONCE: the caches keep no line for them.
+template <int DT, bool ONCE>
+STEP_DEV u4 load_row(const typename Row<DT>::T* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const typename Row<DT>::U*>(p));
+  else return asym_step::load_vec<DT>(p);
 }
 
 // 8 values of a row, wherever it begins.
-template <int DT>
+template <int DT, bool ONCE = false>
 STEP_DEV void load8(const typename Row<DT>::T* p, float* x) {
   if constexpr (DT == ASYMSPEC_BF16) {
-    const u4 v = load_once<DT>(p);
+    const u4 v = load_row<DT, ONCE>(p);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = Row<DT>::get(v, i);
   } else {
-    const u4 v = load_once<DT>(p), w = load_once<DT>(p + 4);
+    const u4 v = load_row<DT, ONCE>(p), w = load_row<DT, ONCE>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]), x[4 + i] = __uint_as_float(w[i]);
   }

@@ -49,7 +49,7 @@ STEP_DEV void each_head(uint32_t from, uint32_t to, Load&& load, Use&& use) {
   if (two) use(2, 0, from + 1), use(3, 1, from + 1);
 }
 
-template <int DT, int BITS>
+template <int DT, int BITS, bool ONCE>
 __global__ __launch_bounds__(kMoveThreads) void write_kernel(MoveArgs A) {
   typedef typename Row<DT>::T T;
   uint32_t group = blockIdx.x;
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kMoveThreads) void write_kernel(MoveArgs A) {
   float f[2 * kMoveHeads][8];
   each_head(
       group * A.heads, min((group + 1) * A.heads, (uint32_t)A.c.heads),
-      [&](int i, int which, uint32_t head) { load8<DT>(which ? v + head * A.v.head : k + head * A.k.head, f[i]); },
+      [&](int i, int which, uint32_t head) { load8<DT, ONCE>(which ? v + head * A.v.head : k + head * A.k.head, f[i]); },
       [&](int i, int which, uint32_t head) {
         uint32_t most = 0;
 #pragma unroll

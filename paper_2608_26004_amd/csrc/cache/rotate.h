@@ -20,8 +20,8 @@ struct RotateArgs {
 };
 
 // VEC: pieces of 16 bytes of each of the pair's sides (or of both, interleaved);
-// else of one pair.
-template <int DT, bool INTER, bool VEC>
+// else of one pair.  ONCE: more than the caches hold, which keep no line of what is read.
+template <int DT, bool INTER, bool VEC, bool ONCE>
 __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs A) {
   typedef typename Row<DT>::T T;
   constexpr int VE = VEC ? Row<DT>::VE : 1;
@@ -62,11 +62,11 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs A) {
     const float2* w = turn + t * (uint32_t)r.n;
     if (piece >= turned) {
       const uint32_t c = 2u * (uint32_t)r.n + (piece - turned) * VE;
-      if constexpr (VEC) asym_step::store_vec<DT>(out + c, asym_step::load_vec<DT>(in + c));
+      if constexpr (VEC) asym_step::store_vec<DT>(out + c, load_row<DT, ONCE>(in + c));
       else out[c] = in[c];
     } else if constexpr (INTER) {
       if constexpr (VEC) {
-        u4 v = asym_step::load_vec<DT>(in + piece * VE);
+        u4 v = load_row<DT, ONCE>(in + piece * VE);
 #pragma unroll
         for (int e = 0; e < VE; e += 2) {
           const float2 cs = w[(piece * VE + e) / 2];
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs A) {
     } else {
       const uint32_t c = piece * VE;
       if constexpr (VEC) {
-        u4 v = asym_step::load_vec<DT>(in + c), z = asym_step::load_vec<DT>(in + c + r.n);
+        u4 v = load_row<DT, ONCE>(in + c), z = load_row<DT, ONCE>(in + c + r.n);
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
           const float2 cs = w[c + e];
