@@ -26,6 +26,7 @@ namespace asym_cache {
 
 constexpr int kAttendThreads = 256;
 constexpr int kUnit = 128;                        // positions of a unit: 32 a wave
+constexpr int kAttendFew = 256;                   // workgroups: one a compute unit
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 constexpr uint32_t kOnes = 0x3F803F80u;           // two bf16
 constexpr float kLog2E = 1.44269504088896340736f;
@@ -33,7 +34,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
   asymspec_attend a;
-  uint32_t* done;       // [runs]: workgroups that have left their part; zero between calls
+  uint32_t* done;       // workgroups that have left their part, of each run; zero between calls
   float* sums;          // [2 workgroups][16 MT][dim]: parts of runs
   f2* stats;            // [2 workgroups][16 MT]: reference, sum
   int group;            // query heads of a head of the cache
@@ -41,6 +42,7 @@ struct AttendArgs {
   int row_tiles;        // of 16 MT rows
   int most;             // positions that a table holds
   int workgroups;
+  float few;            // one over the units below which 256 workgroups are enough
   float c;              // |scale| log2 e, above 0
   uint32_t flip;        // sign bits of a scale below 0, for the queries
   Div by_size, by_group;
@@ -383,7 +385,8 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
     if (w < wave) start += t;
     all += t;
   }
-  const int G = min(A.workgroups, all), me = blockIdx.x;
+  // A part more of a run is as many bytes more for the one that joins them.
+  const int me = blockIdx.x, G = min((float)all * A.few < 1.f ? min(A.workgroups, kAttendFew) : A.workgroups, all);
   int u = 0, end = 0;
   if (me < G) {
     u = (int)((long long)me * all / G);
@@ -719,10 +722,12 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D
       // the workgroups of the run's first and last unit: the last w with w all / G <= unit
       const long long u0 = base + (long long)run * n;
       const int w0 = (int)(((u0 + 1) * G - 1) / all), w1 = (int)(((u0 + n) * G - 1) / all);
-      const int id = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
+      // (neighbours' counters lie in different lines: many workgroups count at once)
+      const int run_id = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
+      uint32_t* const done = A.done + ((run_id & 4095) * 32 + (run_id >> 12));
       if (tid == 0) {
-        is_last = __hip_atomic_fetch_add(&A.done[id], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);
-        if (is_last) __hip_atomic_store(&A.done[id], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        is_last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);
+        if (is_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
       if (is_last) join<DT, D, MT>(A, range, b, head, row0, w0, w1, (long long)w0 * all / G <= u0, lds);

@@ -235,7 +235,9 @@ PyObject* attend_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const OnDevice on(dev);
     out.make(dev);
     void* const stream = stream_of(a[9]);
-    const Tensor ws = attend_workspace(bytes, 4 * std::min<size_t>((size_t)B * H * R, ASYMSPEC_ATTEND_COUNTERS / 4), dev, stream);
+    const size_t runs = (size_t)B * s.cache.heads * ((R * (H / s.cache.heads) + 15) / 16);
+    const size_t counters = std::min<size_t>(128 * runs, ASYMSPEC_ATTEND_COUNTERS);
+    const Tensor ws = attend_workspace(bytes, counters, dev, stream);
     s.out = out.ptr<char>("out", 0, dev);
     if (with_lse) s.lse = out.ptr<float>("lse", 1, dev);
     check(asymspec_attend_cache(&s, ws.data_ptr(), (size_t)ws.numel(), stream));

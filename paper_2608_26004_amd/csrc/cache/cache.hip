@@ -133,6 +133,14 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   if (runs * A->row_tiles > kMostRuns) return 0;
   const long long units = (long long)runs * A->row_tiles * (A->most / kUnit + 2);
   A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
+  // With all workgroups that fit, not one a compute unit, codes stream at 5.2 TB/s
+  // instead of 4.5; a run's join grows by its parts' bytes, at some 40 a ns.  So the
+  // latter where 3.2e-8 us a byte of codes is less than 2.4e-5 us a byte of parts.  (8
+  // requests of 16384 positions in 4 bits, two heads: 16 rows 25 us and 23, 32 rows 39
+  // and 32; with 8 heads, 12 rows 34 and 40.)
+  const double codes = kUnit * 2.0 * (c.dim * c.bits / 8 + c.dim / kBlock);
+  const double parts = (A->workgroups - kAttendFew) * 4.0 * std::min(16 * *tiles, A->rows) * c.dim / (double)(runs * A->row_tiles);
+  A->few = parts > 0 ? (float)(codes / (750 * parts)) : 1e9f;
   const size_t slots = 2 * (size_t)A->workgroups * 16 * *tiles;
   *stats_at = kMostRuns * 4;
   *sums_at = *stats_at + slots * sizeof(f2);
