@@ -344,7 +344,7 @@ STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int
 }
 
 template <int BITS, int DT, int D, int MT>
-__global__ __launch_bounds__(kAttendThreads, attend_waves(DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
+__global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
   typedef Pieces<D> P;
   typedef Codes<BITS, D> C;
   typedef typename Row<DT>::T T;

@@ -17,7 +17,7 @@ static int attend_launch(AttendArgs& A, void* stream) {
 
 template <int D>
 static int attend_tiles(AttendArgs& A, int tiles, void* stream) {
-  constexpr int kMost = attend_most_tiles(kType == ASYMSPEC_BF16, D);
+  constexpr int kMost = attend_most_tiles(kBits, kType == ASYMSPEC_BF16, D);
   if constexpr (kMost >= 4)
     if (tiles == 4) return attend_launch<D, 4>(A, stream);
   if constexpr (kMost >= 2)

@@ -123,7 +123,7 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   if (a.max_blocks < 1 || (long long)a.max_blocks * c.block_size >= (1ll << 31) - 256) return 0;
   A->group = a.q_heads / c.heads;
   A->rows = a.R * A->group;
-  const int most = attend_most_tiles(a.dtype == ASYMSPEC_BF16, c.dim);
+  const int most = attend_most_tiles(c.bits, a.dtype == ASYMSPEC_BF16, c.dim);
   *tiles = 1;
   while (*tiles < most && *tiles * 16 < A->rows) *tiles *= 2;
   A->row_tiles = (A->rows + 16 * *tiles - 1) / (16 * *tiles);
@@ -132,7 +132,7 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   if (runs * ((A->rows + 15) / 16) * (A->most / kUnit + 2) >= ((__int128)1 << 31)) return 0;
   if (runs * A->row_tiles > kMostRuns) return 0;
   const long long units = (long long)runs * A->row_tiles * (A->most / kUnit + 2);
-  A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
+  A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(c.bits, a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
   // With all workgroups that fit, not one a compute unit, codes stream at 5.2 TB/s
   // instead of 4.5; a run's join grows by its parts' bytes, at some 40 a ns.  So the
   // latter where 3.2e-8 us a byte of codes is less than 2.4e-5 us a byte of parts.  (8
