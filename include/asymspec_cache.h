@@ -79,7 +79,7 @@ typedef struct asymspec_heads {
  *                every_row, [B][R].  Any value; a negative one turns back
  *   frequencies  [n] fp64, 8-byte aligned; n in [1, dim / 2]
  * dim in [2, 1024], B, R, q_heads >= 1, q_heads + k_heads at most 4096, B * R below
- * 2^31 - 16.
+ * 2^24.
  */
 typedef struct asymspec_rotate {
   asymspec_heads q, k, q_out, k_out;
@@ -149,15 +149,15 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
  *   q            [B][R][q_heads][dim] (dtype, aligned to an element)
  *   out          [B][R][q_heads][dim] contiguous, 16-byte aligned
  *   lse          [B][R][q_heads] contiguous, or NULL
- *   block_table  [B][max_blocks]; lengths [B] (negative counts as 0);
- *                new_tokens [B] (clamped to [0, R]), or NULL: R
+ *   block_table  [B][max_blocks]; lengths [B] (negative counts as 0, more than
+ *                2^31 - 256 as that); new_tokens [B] (clamped to [0, R]), or NULL: R
  *   window       0 or more
  *   workspace    >= asymspec_attend_workspace_size bytes, 16-byte aligned.  Its
  *                first ASYMSPEC_ATTEND_COUNTERS bytes are zero before its first use
  *                (for a single call the first 128 * B * heads * ceil(R * q_heads /
  *                heads / 16) of them are enough), and each call leaves them so for the
- *                next one, of any shape.  Calls that may run at the same time (replays of captured
- *                ones among them) need distinct ones
+ *                next one, of any shape.  Calls that may run at the same time
+ *                (replays of captured ones among them) need distinct ones
  * The outputs and the workspace overlap no other array.  dim is 64, 96, 128, 192
  * or 256; 1 <= B <= 4096, 1 <= R <= 64; q_heads is a multiple of the cache's
  * heads, at most 64 times as many; max_blocks >= 1, max_blocks * block_size below

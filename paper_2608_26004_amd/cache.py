@@ -148,6 +148,7 @@ def attend_cache(q, cache, block_table, lengths, new_tokens=None, scale=None, wi
     answers from several caches can be joined.  Rows that see nothing and rows from
     new_tokens[b] on are 0, their lse -inf.  What a row does not see has no effect on it,
     whatever is there.  out: the tensor, or with return_lse the two, to write, which
-    overlap no other tensor of the call."""
+    overlap no other tensor of the call.  The workspace is memory kept for the calls of
+    each stream; a captured call has its own, in its graph's memory."""
     return (_s._step or _s._bind()).attend_cache(q, cache, block_table, lengths, new_tokens, scale, window, return_lse,
                                                  out, _s._stream(q))

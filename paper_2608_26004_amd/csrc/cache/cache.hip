@@ -128,10 +128,9 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   while (*tiles < most && *tiles * 16 < A->rows) *tiles *= 2;
   A->row_tiles = (A->rows + 16 * *tiles - 1) / (16 * *tiles);
   A->most = a.max_blocks * c.block_size;
-  const __int128 runs = (__int128)a.B * c.heads;
-  if (runs * ((A->rows + 15) / 16) * (A->most / kUnit + 2) >= ((__int128)1 << 31)) return 0;
-  if (runs * A->row_tiles > kMostRuns) return 0;
-  const long long units = (long long)runs * A->row_tiles * (A->most / kUnit + 2);
+  const long long runs = (long long)a.B * c.heads, n = runs * ((A->rows + 15) / 16), per = A->most / kUnit + 2;
+  if (n > kMostRuns || n * per >= (1ll << 31)) return 0;
+  const long long units = runs * A->row_tiles * per;
   A->workgroups = (int)std::min<long long>(units, kUnits * attend_waves(c.bits, a.dtype == ASYMSPEC_BF16, c.dim, *tiles));
   // With all workgroups that fit, not one a compute unit, codes stream at 5.2 TB/s
   // instead of 4.5; a run's join grows by its parts' bytes, at some 40 a ns.  So the
@@ -160,7 +159,7 @@ int asymspec_rotate_heads(const asymspec_rotate* rotate, void* stream) {
   asymspec_rotate& r = A.r;
   if (!typed(r.dtype) || r.B < 1 || r.R < 1 || r.q_heads < 1 || r.k_heads < 0 || r.q_heads + (long long)r.k_heads > kMostHeads)
     return ASYMSPEC_E_ARG;
-  if (r.dim < 2 || r.dim > 1024 || r.n < 1 || r.n > r.dim / 2 || (long long)r.B * r.R >= kMostTokens) return ASYMSPEC_E_ARG;
+  if (r.dim < 2 || r.dim > 1024 || r.n < 1 || r.n > r.dim / 2 || (long long)r.B * r.R >= (1ll << 24)) return ASYMSPEC_E_ARG;
   if (r.q.at == nullptr || r.q_out.at == nullptr || r.positions == nullptr || r.frequencies == nullptr) return ASYMSPEC_E_ARG;
   if (r.k_heads > 0 && (r.k.at == nullptr || r.k_out.at == nullptr)) return ASYMSPEC_E_ARG;
   if (r.k_heads == 0) r.k = r.k_out = asymspec_heads{};
@@ -223,7 +222,6 @@ int asymspec_rotate_heads(const asymspec_rotate* rotate, void* stream) {
   A.by_pieces = Div(A.pieces);
   A.by_heads = Div((uint32_t)(r.q_heads + r.k_heads));
   const long long grid = (A.tokens + (long long)A.T - 1) / A.T;
-  if (!fits(grid, kRotateThreads)) return ASYMSPEC_E_ARG;
   const size_t lds = (size_t)A.T * r.n * sizeof(float2);
   const bool once = (int64_t)A.tokens * (r.q_heads + r.k_heads) * r.dim * el >= kOnce;
   if (r.dtype == ASYMSPEC_BF16)

@@ -551,6 +551,94 @@ def test_two_streams():
             assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
 
 
+def test_one_workspace_for_calls_of_any_shape():
+    """The C entry point leaves a workspace's counters zero, so that calls of other shapes
+    follow in it; what else is in it does not matter."""
+    import ctypes
+
+    import test_cache_abi as abi
+    lib = abi.library()
+    rng = np.random.default_rng(12)
+    ws = torch.full((40 << 20,), 0x5A, dtype=torch.uint8, device="cuda")
+    counters = 524288
+    ws[:counters] = 0
+    calls = []
+    for B, R, H, Hk, D, bits, S, lengths in ((3, 2, 8, 2, 128, 4, 16, [4000, 0, 900]), (1, 5, 4, 4, 64, 8, 24, [2000]),
+                                             (40, 1, 4, 1, 64, 4, 16, rng.integers(0, 300, 40)), (2, 9, 16, 1, 96, 8, 32, [700, 650])):
+        q, cache, table = attend_inputs(rng, B, R, H, Hk, D, bits, S, "bf16", lengths, garbage=False)
+        q = q.contiguous()
+        c, t, n = on_gpu(cache), gpu(table), gpu(i32(lengths))
+        want = asp.attend_cache(q, c, t, n, return_lse=True)
+        calls.append((q, c, t, n, want, Hk, D, bits, S))
+    for _ in range(3):
+        for q, c, t, n, want, Hk, D, bits, S in calls:
+            out, lse = (torch.full_like(x, 7) for x in want)
+            a = abi.Attend(cache=abi.Cache(*(x.data_ptr() for x in c), c[0].shape[0], Hk, S, D, bits),
+                           q=abi.Heads(q.data_ptr(), *q.stride()[:3]), out=out.data_ptr(), lse=lse.data_ptr(),
+                           block_table=t.data_ptr(), lengths=n.data_ptr(), new_tokens=None, scale=D ** -0.5, window=0, dtype=0,
+                           B=q.shape[0], R=q.shape[1], q_heads=q.shape[2], max_blocks=t.shape[1])
+            assert lib.asymspec_attend_workspace_size(ctypes.byref(a)) <= ws.numel()
+            st = torch.cuda.current_stream().cuda_stream
+            assert lib.asymspec_attend_cache(ctypes.byref(a), ws.data_ptr(), ws.numel(), st) == 0
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+            assert not ws[:counters].any()
+
+
+def test_a_growing_workspace():
+    """A call that needs a larger workspace while calls in the smaller one are still on
+    their way, on a stream of its own."""
+    rng = np.random.default_rng(13)
+    small = attend_inputs(rng, 2, 1, 2, 1, 64, 4, 16, "bf16", [900, 300], garbage=False)
+    large = attend_inputs(rng, 4, 4, 16, 2, 256, 4, 16, "bf16", [3000, 900, 2000, 5], garbage=False)
+    args = [(q, on_gpu(c), gpu(t), gpu(i32(n))) for (q, c, t), n in ((small, [900, 300]), (large, [3000, 900, 2000, 5]))]
+    want = [asp.attend_cache(*a) for a in args]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = [asp.attend_cache(*args[0]) for _ in range(30)] + [asp.attend_cache(*args[1])] + \
+              [asp.attend_cache(*args[0]) for _ in range(5)]
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert torch.equal(g, want[i == 30]), i
+
+
+def test_attend_most_requests():
+    """4096 requests of one position, some of none, and rows of all of them."""
+    rng = np.random.default_rng(14)
+    B, S = 4096, 16
+    lengths = rng.integers(0, 2, B)
+    new = rng.integers(0, 2, B)
+    q, cache, table = attend_inputs(rng, B, 1, 1, 1, 64, 8, S, "bf16", lengths, garbage=False)
+    check_attend(q, cache, table, lengths, 8, new_tokens=new)
+
+
+@pytest.mark.parametrize("bits,dtype", [(4, "bf16"), (8, "fp32")])
+def test_attend_blocks_that_requests_share(bits, dtype):
+    """A prefix that is in the cache once, in several requests' tables."""
+    rng = np.random.default_rng(15)
+    S, lengths = 16, [200, 200, 200]
+    q, cache, table = attend_inputs(rng, 3, 2, 4, 2, 64, bits, S, dtype, lengths)
+    table[1, :8] = table[0, :8]
+    table[2, :11] = table[0, :11]
+    check_attend(q, cache, table, lengths, bits)
+
+
+def test_lse_joins_two_caches():
+    """Answers over the two halves of a context, joined by their lse, are the answer over it
+    all, within the roundings of bf16 answers."""
+    rng = np.random.default_rng(16)
+    q, cache, table = attend_inputs(rng, 2, 1, 4, 2, 64, 8, 16, "fp32", [255, 255])
+    c = on_gpu(cache)
+    whole, lse = asp.attend_cache(q, c, gpu(table), gpu(i32([255, 255])), return_lse=True)
+    parts = [asp.attend_cache(q, c, gpu(t), gpu(i32([127, 127])), return_lse=True) for t in (table[:, :8], table[:, 8:])]
+    l = torch.stack([p[1] for p in parts]).double()
+    w = torch.softmax(l, 0)[..., None]
+    got = (w * torch.stack([p[0] for p in parts]).double()).sum(0)
+    # fp32 answers within about 100 u of sums of values below 8; lse within 100 u
+    assert (got - whole.double()).abs().max() < 2 * 100 * 2.0 ** -24 * 8
+    assert (torch.logsumexp(l, 0) - lse.double()).abs().max() < 100 * 2.0 ** -24 * 16
+
+
 def test_writes_count_as_versions():
     x = torch.randn(2, 1, 1, 32, device="cuda")
     cache = asp.new_cache(2, 1, 2, 32, 8)
