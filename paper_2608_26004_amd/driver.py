@@ -27,6 +27,12 @@ steps: penalties, biases and masks shape the rows (``shape_logits``), the drafte
 draws on the GPU (``draw_tokens``), what a step commits joins the histories there
 (``commit_tokens``), and the stand-in models keep their context per position in a
 paged store, as a model keeps its keys and values (``plan_slots``).
+
+``CachedDecoder`` is that loop with keys and values: each token has a query, a key
+and a value (random tables), and what a row's attention over a paged cache in 8 or 4
+bits answers chooses the logit row (``rotate_heads``, ``write_cache``,
+``attend_cache``).  The drafter attends to its full context token by token, its
+compressed view and the verifier to the last ``window`` positions, K + 1 rows at once.
 """
 
 from __future__ import annotations
@@ -277,41 +283,62 @@ class ResidentDecoder:
                                draft_tokens=drafts if drafts.shape[1] else None, mask=self.mask, mask_index=index,
                                **self.shape)
 
+    # What a subclass keeps for a position, other than its context's hash: the table rows
+    # that the views' logits are, and what a step leaves behind.
+    def _begin(self):
+        """(slots of the step's K + 1 positions, short) and the state of the step."""
+        slots, short = self._place(self.lengths + 1, self.K + 1)
+        self.slots = self._torch.where(slots < 0, len(self.store) - 1, slots)
+        self.hs = self._torch.empty(self.B, self.K + 1, dtype=self._torch.int64, device=self.device)
+        return short
+
+    def _drafter_rows(self, i, token):
+        """Table rows of the drafter's full view of position i, behind `token` (None: i = 0)."""
+        h = self.store[self.at] if i == 0 else (self.hs[:, i - 1] * _MUL + token + 1) & _MASK
+        if i > 0:
+            self.store[self.slots[:, i - 1]] = h
+        self.hs[:, i] = h
+        return h % self.m.R
+
+    def _view_rows(self):
+        """Table rows of the verifier and of the drafter's compressed view, [B, K + 1] each."""
+        rows = self.hs % self.m.R
+        return rows, rows
+
+    def _end(self, live, j, nxt, tokens, n):
+        torch, slots = self._torch, self.slots
+        emitted = (self.hs.gather(1, j)[:, 0] * _MUL + nxt + 1) & _MASK
+        self.store[torch.where(live, slots.gather(1, j)[:, 0], len(self.store) - 1)] = emitted
+        last = slots.gather(1, (n.long() - 1).clamp_min(0)[:, None])[:, 0]
+        self.at = torch.where(n > 0, last, self.at)
+
     def step(self):
         torch, asp, B, K, m = self._torch, self._asp, self.B, self.K, self.m
         dev = self.device
         ud = torch.from_numpy(self.rng.random((B, K)).astype(np.float32)).to(dev, non_blocking=True)
         u = torch.from_numpy(self.rng.random((B, K + 1), dtype=np.float32)).to(dev, non_blocking=True)
-        slots, short = self._place(self.lengths + 1, K + 1)
-        slots = torch.where(slots < 0, len(self.store) - 1, slots)
+        short = self._begin()
         a = torch.empty(B, K + 1, m.V, dtype=m.dev[1].dtype, device=dev)
         d = torch.empty(B, K, dtype=torch.int32, device=dev)
         q = torch.empty(B, K, dtype=torch.float32, device=dev)
-        hs = torch.empty(B, K + 1, dtype=torch.int64, device=dev)
-        h = self.store[self.at]
         for i in range(K + 1):
-            hs[:, i] = h
-            a[:, i] = m.dev[1].index_select(0, h % m.R)
+            a[:, i] = m.dev[1].index_select(0, self._drafter_rows(i, d[:, i - 1] if i > 0 else None))
             self._shape(a[:, i:i + 1], d[:, :i], i)
             if i < K:
                 asp.draw_tokens(a[:, i], self.tau, ud[:, i], out=(d[:, i], q[:, i]))
-                h = (h * _MUL + d[:, i] + 1) & _MASK
-                self.store[slots[:, i]] = h
-        rows = (hs % m.R).view(-1)
-        t, b = (m.dev[k].index_select(0, rows).view(B, K + 1, m.V) for k in (0, 2))
+        t, b = (m.dev[k].index_select(0, rows.reshape(-1)).view(B, K + 1, m.V)
+                for k, rows in zip((0, 2), self._view_rows()))
         for x in (t, b):
             self._shape(x, d, 0)
         acc, nxt, _ = asp.fuse_verify(t, a, b, d, q, u, self.tau, **self.kw)
         acc = torch.where(short != 0, -1, acc)                 # no room: the step does not count
         live = (acc >= 0) & (self.finished == 0)
         _, _, tokens, n = asp.commit_tokens(acc, nxt, d, self.history, self.lengths, self.finished, self.stop,
-                                            out=(self.lengths, self.finished, torch.empty_like(hs, dtype=torch.int32),
+                                            out=(self.lengths, self.finished,
+                                                 torch.empty(B, K + 1, dtype=torch.int32, device=dev),
                                                  torch.empty_like(acc)))
         j = acc.clamp_min(0).long()[:, None]
-        emitted = (hs.gather(1, j)[:, 0] * _MUL + nxt + 1) & _MASK
-        self.store[torch.where(live, slots.gather(1, j)[:, 0], len(self.store) - 1)] = emitted
-        last = slots.gather(1, (n.long() - 1).clamp_min(0)[:, None])[:, 0]
-        self.at = torch.where(n > 0, last, self.at)
+        self._end(live, j, nxt, tokens, n)
         ok = live.long()
         self.counts += torch.stack([(ok * j[:, 0]).sum(), (ok * (j[:, 0] + (acc < K))).sum(), n.sum()])
         self.request_steps += ok.sum()
@@ -332,6 +359,81 @@ class ResidentDecoder:
                 "tokens": committed, "finished": int((self.finished != 0).sum())}
 
 
+class AttentionModels(TableModels):
+    """Stand-ins whose logit rows are chosen by attention: a token has a query of `heads`
+    and a key and value of `kv_heads` heads (random tables, float32), and the row behind a
+    position is that of the anchor nearest to the position's answer (the largest
+    product)."""
+
+    def __init__(self, V: int, R: int = 512, heads: int = 8, kv_heads: int = 2, dim: int = 64, device=None, seed: int = 0,
+                 **kw):
+        import torch
+        import paper_2608_26004_amd as asp
+        super().__init__(V, R=R, device=device, seed=seed, **kw)
+        if device is None:
+            raise ValueError("the attention's tables need a device")
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, dim
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        self.qkv = torch.randn(V, heads + 2 * kv_heads, dim, device=device, generator=g)
+        self.anchors = torch.randn(R, heads * dim, device=device, generator=g)
+        self.frequencies = asp.rotary_frequencies(dim, device=device)
+
+    def rows(self, answers):
+        """Table rows of answers [B, n, heads, dim]."""
+        return (answers.flatten(2) @ self.anchors.T).argmax(-1)
+
+
+class CachedDecoder(ResidentDecoder):
+    """ResidentDecoder over AttentionModels: the drafter's keys and values in `bits` bits,
+    the verifier's in `verifier_bits`, in the same blocks.  The tokens of a request stand
+    at the positions of its history, behind its start token; a step writes the last
+    committed token and its drafts, and what is rejected is written over by the next one.
+
+    window: positions that the verifier and the drafter's compressed view see (0: all)."""
+
+    def __init__(self, models: AttentionModels, B: int, K: int, temperature, bits: int = 4, verifier_bits: int = 8,
+                 window: int = 0, **kw):
+        super().__init__(models, B, K, temperature, **kw)
+        torch, asp, m = self._torch, self._asp, models
+        blocks = len(self.ring)
+        self.caches = [asp.new_cache(blocks, m.kv_heads, self.block_size, m.dim, n, device=self.device)
+                       for n in (bits, verifier_bits)]
+        self.window = window
+        self.last = (torch.arange(B, device=self.device) % m.V).int()       # the start tokens
+
+    def _begin(self):
+        m = self.m
+        self.slots, short = self._place(self.lengths, self.K + 1)
+        self.turned = self._torch.empty(self.B, self.K + 1, m.heads + m.kv_heads, m.dim, device=self.device)
+        self.values = self._torch.empty(self.B, self.K + 1, m.kv_heads, m.dim, device=self.device)
+        self.a_rows = []
+        return short
+
+    def _drafter_rows(self, i, token):
+        asp, m = self._asp, self.m
+        x = m.qkv[(self.last if i == 0 else token).long()][:, None]
+        at = self.lengths + i
+        q, k = self.turned[:, i:i + 1].split([m.heads, m.kv_heads], 2)
+        asp.rotate_heads(x[:, :, :m.heads], x[:, :, m.heads:m.heads + m.kv_heads], at, m.frequencies, out=(q, k))
+        self.values[:, i] = x[:, 0, m.heads + m.kv_heads:]
+        asp.write_cache(k, self.values[:, i:i + 1], self.slots[:, i:i + 1].contiguous(), self.caches[0])
+        self.a_rows.append(m.rows(asp.attend_cache(q, self.caches[0], self.table, at))[:, 0])
+        return self.a_rows[-1]
+
+    def _view_rows(self):
+        asp, m = self._asp, self.m
+        q, k = self.turned.split([m.heads, m.kv_heads], 2)
+        asp.write_cache(k, self.values, self.slots, self.caches[1])
+        t, b = (m.rows(asp.attend_cache(q, c, self.table, self.lengths, window=self.window)) for c in reversed(self.caches))
+        self.t_rows, self.b_rows = t, b
+        return t, b
+
+    def _end(self, live, j, nxt, tokens, n):
+        last = tokens.gather(1, (n.long() - 1).clamp_min(0)[:, None])[:, 0]
+        self.last = self._torch.where(n > 0, last, self.last)
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description="multi-step speculative decoding over stand-in models")
     ap.add_argument("--B", type=int, default=8)
@@ -350,18 +452,29 @@ def main(argv=None):
     ap.add_argument("--resident", action="store_true", help="draft, commit and place on the GPU")
     for name in ("repetition", "frequency", "presence"):
         ap.add_argument("--" + name, type=float, default=None, help="penalty (with --resident)")
+    ap.add_argument("--cache", type=int, choices=[4, 8], default=None,
+                    help="keys and values of the drafter in so many bits (with --resident)")
+    ap.add_argument("--window", type=int, default=0, help="positions that the compressed views see (with --cache)")
     args = ap.parse_args(argv)
     penalties = {n: getattr(args, n) for n in ("repetition", "frequency", "presence")}
     if not args.resident and any(v is not None for v in penalties.values()):
         ap.error("penalties need --resident")
+    if args.cache is not None and not args.resident:
+        ap.error("--cache needs --resident")
+    if args.window and args.cache is None:
+        ap.error("--window needs --cache")
     import torch
     dev = torch.device("cuda")
-    models = TableModels(args.V, R=args.R, rho=args.rho, dtype=args.dtype, seed=args.seed, device=dev)
+    kind = TableModels if args.cache is None else AttentionModels
+    models = kind(args.V, R=args.R, rho=args.rho, dtype=args.dtype, seed=args.seed, device=dev)
     gm = {"cda": 0, "fixed": 1, "kl": 2, "lambda": 3}[args.gate]
     if args.resident:
-        dec = ResidentDecoder(models, args.B, args.K, args.tau, beta=args.beta, gamma=args.gamma, gate_mode=gm,
-                              seed=args.seed + 1, early_exit=args.early_exit,
-                              max_tokens=args.steps * (args.K + 1) + 1, **penalties)
+        kw = dict(beta=args.beta, gamma=args.gamma, gate_mode=gm, seed=args.seed + 1, early_exit=args.early_exit,
+                  max_tokens=args.steps * (args.K + 1) + 1, **penalties)
+        if args.cache is None:
+            dec = ResidentDecoder(models, args.B, args.K, args.tau, **kw)
+        else:
+            dec = CachedDecoder(models, args.B, args.K, args.tau, bits=args.cache, window=args.window, **kw)
     else:
         dec = SpecDecoder(models, args.B, args.K, args.tau, beta=args.beta, gamma=args.gamma,
                           gate_mode=gm, seed=args.seed + 1, device=dev, early_exit=args.early_exit)
@@ -375,6 +488,8 @@ def main(argv=None):
                 "rho": args.rho, "gate": args.gate, "early_exit": args.early_exit, "wall_s": wall})
     if args.resident:
         rep.update({"resident": True, **{k: v for k, v in penalties.items() if v is not None}})
+    if args.cache is not None:
+        rep.update({"cache_bits": args.cache, "window": args.window})
     print(json.dumps(rep))
 
 
