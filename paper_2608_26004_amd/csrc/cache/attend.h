@@ -483,22 +483,24 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       // scores of positions 16 a + 4 i + h
       f4 s[MT][2];
 #pragma unroll
-      for (int a = 0; a < 2; ++a) {
+      for (int m = 0; m < MT; ++m) s[m][0] = s[m][1] = f4{0, 0, 0, 0};
+      count<P::N>([&](auto pc) {
+        constexpr int w = P::width(pc), base_ch = P::base(pc);
+        const float scale[2] = {scale_of(c.key_scale[0][pc]), scale_of(c.key_scale[1][pc])};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) s[m][a] = f4{0, 0, 0, 0};
-        count<P::N>([&](auto pc) {
-          constexpr int w = P::width(pc), base_ch = P::base(pc);
-          const float scale = scale_of(c.key_scale[a][pc]);
+        for (int st = 0; st < w / 32; ++st) {
+          u4 k[2];
 #pragma unroll
-          for (int st = 0; st < w / 32; ++st) {
-            const u4 k = decode8<BITS>(&c.key[a][base_ch * BITS / 128 + st * (BITS / 4)], scale);
+          for (int a = 0; a < 2; ++a) k[a] = decode8<BITS>(&c.key[a][base_ch * BITS / 128 + st * (BITS / 4)], scale[a]);
+          // (two sums in turn: a matrix instruction waits for the one before it on its own)
+#pragma unroll
+          for (int x = 0; x < kParts; ++x)
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-              for (int x = 0; x < kParts; ++x) s[m][a] = mfma(k, q[m][x][base_ch / 32 + st], s[m][a]);
-          }
-        });
-      }
+              for (int a = 0; a < 2; ++a) s[m][a] = mfma(k[a], q[m][x][base_ch / 32 + st], s[m][a]);
+        }
+      });
       // the largest of the scale bytes
       uint32_t most_key = 0, most_val = 0;
 #pragma unroll
@@ -629,9 +631,9 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
             odd[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302u);
           }
 #pragma unroll
-          for (int m = 0; m < MT; ++m)
+          for (int k = 0; k < kProb; ++k)
 #pragma unroll
-            for (int k = 0; k < kProb; ++k) {
+            for (int m = 0; m < MT; ++m) {
               acc[m][base_ch / 16 + 2 * e2] = mfma(even, prob[m][k], acc[m][base_ch / 16 + 2 * e2]);
               acc[m][base_ch / 16 + 2 * e2 + 1] = mfma(odd, prob[m][k], acc[m][base_ch / 16 + 2 * e2 + 1]);
             }

@@ -17,11 +17,8 @@ static int attend_launch(AttendArgs& A, void* stream) {
 
 template <int D>
 static int attend_tiles(AttendArgs& A, int tiles, void* stream) {
-  constexpr int kMost = attend_most_tiles(kBits, kType == ASYMSPEC_BF16, D);
-  if constexpr (kMost >= 4)
-    if (tiles == 4) return attend_launch<D, 4>(A, stream);
-  if constexpr (kMost >= 2)
-    if (tiles == 2) return attend_launch<D, 2>(A, stream);
+  if constexpr (attend_most_tiles(kBits, kType == ASYMSPEC_BF16, D) > 1)
+    if (tiles > 1) return attend_launch<D, 2>(A, stream);
   return attend_launch<D, 1>(A, stream);
 }
 

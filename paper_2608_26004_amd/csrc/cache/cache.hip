@@ -123,9 +123,7 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   if (a.max_blocks < 1 || (long long)a.max_blocks * c.block_size >= (1ll << 31) - 256) return 0;
   A->group = a.q_heads / c.heads;
   A->rows = a.R * A->group;
-  const int most = attend_most_tiles(c.bits, a.dtype == ASYMSPEC_BF16, c.dim);
-  *tiles = 1;
-  while (*tiles < most && *tiles * 16 < A->rows) *tiles *= 2;
+  *tiles = A->rows > 16 ? attend_most_tiles(c.bits, a.dtype == ASYMSPEC_BF16, c.dim) : 1;
   A->row_tiles = (A->rows + 16 * *tiles - 1) / (16 * *tiles);
   A->most = a.max_blocks * c.block_size;
   const long long runs = (long long)a.B * c.heads, n = runs * ((A->rows + 15) / 16), per = A->most / kUnit + 2;
