@@ -1,20 +1,35 @@
 // attend_cache: softmax(scale q k^T) v over a paged cache in 8 or 4 bits, in one pass.
 //
 // Work is cut along the cache: a unit is 128 positions of one head of the cache, for
-// all rows of the step and all query heads that read it (16 MT of these rows at a
-// time).  The units of all requests form one list, which the workgroups share evenly,
-// whatever the requests' lengths: each takes a run of neighbouring units, of which
-// each of its four waves takes 32 positions.  A wave keeps a running reference and sum
-// for each row, so that nothing is exchanged until a run ends; there the waves' parts
-// meet in LDS, and parts of different workgroups in memory, where the last one to leave
-// its part joins them (in the workgroups' order, whoever is last).
+// all rows of the step and all query heads that read it (16 or 32 of these rows at a
+// time: a row tile, and a run is what a request's head has for one).  A workgroup takes
+// neighbouring units of a run, of which each of its four waves has 32 positions.  A wave
+// keeps a running reference and sum for each row, so that nothing is exchanged until the
+// units end; there the waves' parts meet in LDS, and parts of different workgroups in
+// memory, where the last one to leave its part joins them (in the workgroups' order,
+// whoever is last, so that the answer is always the same).
 //
-// Both products run on 16x16x32 bf16 matrix instructions.  For the scores a lane
-// decodes what it loaded, with the order of the channels permuted alike on both sides
-// so that a lane's piece of a key is contiguous; the scores come out as the second
-// product's operand needs its probabilities (one row a lane, four positions in a row),
-// so that those never move between lanes.  A lane loads the same channels of eight
-// positions of the values and pairs them by byte permutes.
+// Both products run on 16x16x32 bf16 matrix instructions: a code times its scale is
+// exact in bf16.  For the scores a lane decodes what it loaded, with the order of the
+// channels permuted alike on both sides so that a lane's piece of a key is contiguous;
+// the scores come out as the second product's operand needs its probabilities (one row a
+// lane, eight positions), so that those never move between lanes.  A lane loads the same
+// channels of eight positions of the values and pairs them by byte permutes.  The sum of
+// the probabilities is a product with ones, of the parts that meet the values.
+//
+// Bound by memory where requests are long: 128 requests of 7 x 4 rows and 4096 to 8192
+// positions, 8 heads of 128 channels in 8 bits, 1.67 GB, take 288 us (5.8 TB/s; a copy
+// reaches 5.1), two of 131072 to 262144 positions in 4 bits 93 (4.6 TB/s).  The loads
+// alone take 267 and 79 us there, the arithmetic alone 200 and 70: decoding and the
+// exponentials keep the vector units 65% busy, the matrix ones 27%.  Where work is small the
+// ends weigh as much: 8 requests of 8192 to 16384 positions, 12 rows, 32.5 us, of it 5 the
+// waves' parts, 4 the join; one row over 2048 positions 9.7, of it 4 to 5 the join.
+//
+// What was slower: codes loaded ahead in registers (they spill); two sets of 32 positions
+// in flight (104 us for 99 in the second case); eight waves a workgroup (301 for 295 in the first);
+// parts made visible by an agent's fences (100 us more a call).  The scaled
+// matrix instructions that take codes as they are would save the decoding of keys, but their sums
+// hold only 2^-13 of the terms.
 
 #ifndef ASYMSPEC_CACHE_ATTEND_H_
 #define ASYMSPEC_CACHE_ATTEND_H_
@@ -343,6 +358,12 @@ STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int
   }
 }
 
+// The whole part of a / b, the same in all lanes; a is below 2^42.  (A quotient that is not
+// whole is 1 / b and more below the next whole number, 2^-42 of it: a rounding does not reach it.)
+STEP_DEV int over(double a, int b) { return __builtin_amdgcn_readfirstlane((int)(a / b)); }
+
+STEP_DEV int pieces_of(int units, int most) { return most == 1 ? units : (units + most - 1) / most; }
+
 template <int BITS, int DT, int D, int MT>
 __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
   typedef Pieces<D> P;
@@ -358,7 +379,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   __shared__ __align__(16) uint8_t lds[kLds];
   float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
-  __shared__ int totals[4], found[4], is_last;
+  __shared__ int totals[3][4], found[4], list[2], shared_by[3], is_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int j = lane & 15, h = lane >> 4;
@@ -367,36 +388,61 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   // The requests' first units in the list, and the request of this workgroup's first one.
   const int each = (A.a.B + kAttendThreads - 1) / kAttendThreads;
   const Range lane_first(A, min(tid * each, A.a.B - 1));    // (a thread's only one, up to 256 requests)
-  int mine = tid * each < A.a.B ? lane_first.units * per_unit : 0;
-  for (int i = 1; i < each; ++i)
-    if (tid * each + i < A.a.B) mine += Range(A, tid * each + i).units * per_unit;
-  int upto = mine;
+  const int me = blockIdx.x;
+  int all = 0, items = 0, G = 0, even = 0;
+  // Where there are workgroups for all runs if each has at most `most` units of one, that
+  // is what they have; else (0) even shares of the list, which begin and end within runs and cost
+  // a workgroup the ends of two.  (8 requests of 8192 to 16384 positions 32.5 us, with even
+  // shares 33.4; windows of 1024 positions, 32 requests of 16 heads in fp32, 16.8 and 17.8.)
+  int most = 0, mine = 0, start = 0;
+#pragma nounroll
+  for (int i = 0; i < 3; ++i) {
+    const int m = i == 0 ? 1 : i == 1 ? even : even + 1 + even / 16;
+    int own = tid * each < A.a.B ? pieces_of(lane_first.units, m) * per_unit : 0;
+    for (int k = 1; k < each; ++k)
+      if (tid * each + k < A.a.B) own += pieces_of(Range(A, tid * each + k).units, m) * per_unit;
+    int upto = own;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int below = __shfl_up(upto, d);
-    if (lane >= d) upto += below;
-  }
-  if (lane == 63) totals[wave] = upto;
-  __syncthreads();
-  int start = upto - mine, all = 0;
+    for (int d = 1; d < 64; d *= 2) {
+      const int below = __shfl_up(upto, d);
+      if (lane >= d) upto += below;
+    }
+    if (lane == 63) totals[i][wave] = upto;
+    __syncthreads();
+    int ahead = upto - own;
+    items = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int t = totals[w];
-    if (w < wave) start += t;
-    all += t;
+    for (int w = 0; w < 4; ++w) {
+      const int t = totals[i][w];
+      if (w < wave) ahead += t;
+      items += t;
+    }
+    items = __builtin_amdgcn_readfirstlane(items);
+    if (i == 0) {
+      all = items;
+      // a part more of a run is as many bytes more for the one that joins them
+      G = __builtin_amdgcn_readfirstlane(min((float)all * A.few < 1.f ? min(A.workgroups, kAttendFew) : A.workgroups, all));
+      even = G > 0 ? over((double)all + G - 1, G) : 0;
+    } else if (items > G) {
+      continue;
+    } else {
+      most = m;
+    }
+    mine = own;
+    start = ahead;
+    if (even <= 1 || i > 0) break;
   }
-  // A part more of a run is as many bytes more for the one that joins them.
-  const int me = blockIdx.x, G = min((float)all * A.few < 1.f ? min(A.workgroups, kAttendFew) : A.workgroups, all);
   int u = 0, end = 0;
-  if (me < G) {
-    u = (int)((long long)me * all / G);
-    end = (int)((long long)(me + 1) * all / G);
+  if (most == 0 && me < G) {
+    u = over((double)me * all, G);
+    end = over((double)(me + 1) * all, G);
   }
-  if (u >= start && u < start + mine) {
+  const int item = most > 0 ? me : u;
+  if (item >= start && item < start + mine) {
     Range r = lane_first;
     int b = tid * each;
-    while (u >= start + r.units * per_unit) {
-      start += r.units * per_unit;
+    for (int n; item >= start + (n = pieces_of(r.units, max(most, 1)) * per_unit);) {
+      start += n;
       r = Range(A, ++b);
     }
     found[0] = b, found[1] = start, found[2] = r.len, found[3] = r.fresh;
@@ -404,6 +450,18 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
   Range range(A, __builtin_amdgcn_readfirstlane(found[2]), __builtin_amdgcn_readfirstlane(found[3]));
+  // (what a run's end needs waits in LDS: its workgroups, and whether its first one begins with it)
+  if (most > 0 && me < items) {
+    const int n = range.units, pieces = __builtin_amdgcn_readfirstlane(pieces_of(n, most));
+    const int run = over(me - base, pieces), piece = (me - base) - run * pieces;
+    if (tid == 0) shared_by[0] = me - piece, shared_by[1] = me - piece + pieces - 1, shared_by[2] = 1;
+    base = 0;                                             // (units of this request)
+    u = run * n + over((double)n * piece, pieces);
+    end = run * n + over((double)n * (piece + 1), pieces);
+  } else if (tid == 0) {
+    list[0] = all, list[1] = G;
+  }
+  const bool alone = most > 0;
 
   while (u < end) {
     const int n = range.units;
@@ -412,7 +470,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       range = Range(A, ++b);
       continue;
     }
-    const int run = (u - base) / n, from = (u - base) - run * n, to = min(n, from + (end - u));
+    const int run = over(u - base, n), from = (u - base) - run * n, to = min(n, from + (end - u));
     const int head = run / A.row_tiles, row0 = (run - head * A.row_tiles) * (16 * MT);
     u += to - from;
 
@@ -718,21 +776,26 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       }
     }
     // (a part is in memory before it is counted, whichever wave stored it)
-    if (!complete) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (!complete) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (!alone && tid == 0) {
+        // the workgroups of its first and last unit: the last w with w all / G <= unit
+        const int all = list[0], G = list[1], u0 = base + run * n, w0 = over((u0 + 1.) * G - 1, all);
+        shared_by[0] = w0, shared_by[1] = over(((double)u0 + n) * G - 1, all), shared_by[2] = over((double)w0 * all, G) <= u0;
+      }
+    }
     __syncthreads();                                      // (codes go there again)
     if (!complete) {
-      // the workgroups of the run's first and last unit: the last w with w all / G <= unit
-      const long long u0 = base + (long long)run * n;
-      const int w0 = (int)(((u0 + 1) * G - 1) / all), w1 = (int)(((u0 + n) * G - 1) / all);
       // (neighbours' counters lie in different lines: many workgroups count at once)
       const int run_id = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
       uint32_t* const done = A.done + ((run_id & 4095) * 32 + (run_id >> 12));
       if (tid == 0) {
-        is_last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(w1 - w0);
+        is_last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+                  (uint32_t)(shared_by[1] - shared_by[0]);
         if (is_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
-      if (is_last) join<DT, D, MT>(A, range, b, head, row0, w0, w1, (long long)w0 * all / G <= u0, lds);
+      if (is_last) join<DT, D, MT>(A, range, b, head, row0, shared_by[0], shared_by[1], shared_by[2], lds);
       __syncthreads();
     }
   }

@@ -393,6 +393,21 @@ def test_attend_long(bits, S):
     check_attend(q, cache, table, lengths, bits, window=3000, new_tokens=[2, 1, 2, 0, 1])
 
 
+@pytest.mark.parametrize("bits,dtype", [(4, "bf16"), (8, "fp32")])
+@pytest.mark.parametrize("units,window", [
+    ([11] * 8, 0),                          # as many units each: pieces of runs, and whole ones
+    ([4] * 8 + [8] * 8, 500),
+    ([17, 15] * 4, 0),                      # no even pieces: those of one more unit
+    ([2, 3] * 40, 0),                       # more runs than workgroups
+    ([64] + [1] * 30 + [0, 2], 0)])         # one long request among short ones
+def test_attend_shares(bits, dtype, units, window):
+    """How units are shared among 512 workgroups, for lengths at and around whole units."""
+    rng = np.random.default_rng(sum(units))
+    lengths = np.array([max(0, 128 * n - int(rng.choice([2, 3, 65]))) for n in units])
+    q, cache, table = attend_inputs(rng, len(units), 2, 8, 8, 128, bits, 32, dtype, lengths)
+    check_attend(q, cache, table, lengths, bits, window=window)
+
+
 def test_attend_many_requests():
     rng = np.random.default_rng(9)
     B = 700
