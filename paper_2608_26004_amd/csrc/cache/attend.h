@@ -3,7 +3,8 @@
 // Work is cut along the cache: a unit is 128 positions of one head of the cache, for
 // all rows of the step and all query heads that read it (16 or 32 of these rows at a
 // time: a row tile, and a run is what a request's head has for one).  A workgroup takes
-// neighbouring units of a run, of which each of its four waves has 32 positions.  A wave
+// neighbouring units of a run, of which each of its four waves has 32 positions (or, where
+// runs are many and short, each wave takes whole runs by itself).  A wave
 // keeps a running reference and sum for each row, so that nothing is exchanged until the
 // units end; there the waves' parts meet in LDS, and parts of different workgroups in
 // memory, where the last one to leave its part joins them (in the workgroups' order,
@@ -23,7 +24,7 @@
 // alone take 267 and 79 us there, the arithmetic alone 200 and 70: decoding and the
 // exponentials keep the vector units 65% busy, the matrix ones 27%.  Where work is small the
 // ends weigh as much: 8 requests of 8192 to 16384 positions, 12 rows, 32.5 us, of it 5 the
-// waves' parts, 4 the join; one row over 2048 positions 9.7, of it 4 to 5 the join.
+// waves' parts, 4 the join; one row over 2048 positions 10, of it 4 to 5 the join.
 //
 // What was slower: codes loaded ahead in registers (they spill); two sets of 32 positions
 // in flight (104 us for 99 in the second case); eight waves a workgroup (301 for 295 in the first);
@@ -89,6 +90,17 @@ struct Range {
 STEP_DEV float lanes_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// f over the lanes up to each one, of numbers from 0 on.
+template <class F>
+STEP_DEV int lanes_upto(int x, F&& f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // a row's lanes
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // the row's before it
+  return f(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));   // the half's
 }
 
 STEP_DEV uint32_t bf_pair(float a, float b) {
@@ -249,8 +261,16 @@ struct Codes {
   }
 };
 
-// Four channels of a row from its sums, and its lse.
-template <int DT>
+// The thread's number, from its wave's: neither it nor what is computed from it waits in
+// registers.
+STEP_DEV int thread_again(int wave) {
+  int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0));
+  asm volatile("" : "+v"(lane));
+  return 64 * wave + lane;
+}
+
+// N (2 or 4) channels of a row from its sums, and its lse.
+template <int DT, int N = 4>
 STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int ch, float ref, float sum, const f4& o) {
   typedef typename Row<DT>::T T;
   const int64_t at = ((int64_t)b * A.a.R + r) * A.a.q_heads + q_head;
@@ -258,9 +278,11 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
   const float over = 1.f / sum;
   float y[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = none ? 0.f : o[e] * over;
+  for (int e = 0; e < N; ++e) y[e] = none ? 0.f : o[e] * over;
   T* out = (T*)A.a.out + at * dim + ch;
-  if constexpr (DT == ASYMSPEC_BF16) *(u2*)out = u2{bf_pair(y[0], y[1]), bf_pair(y[2], y[3])};
+  if constexpr (DT == ASYMSPEC_BF16 && N == 2) *(uint32_t*)out = bf_pair(y[0], y[1]);
+  else if constexpr (DT == ASYMSPEC_BF16) *(u2*)out = u2{bf_pair(y[0], y[1]), bf_pair(y[2], y[3])};
+  else if constexpr (N == 2) *(f2*)out = f2{y[0], y[1]};
   else *(f4*)out = f4{y[0], y[1], y[2], y[3]};
   if (ch == 0 && A.a.lse != nullptr) A.a.lse[at] = none ? -INFINITY : (ref + log2f(sum)) * kLn2;
 }
@@ -281,11 +303,10 @@ STEP_DEV T left(const T* p) { return __builtin_nontemporal_load(p); }
 // take as long: what counts is that this code, which runs once, is short).
 template <int DT, int D, int MT>
 STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, int w0, int w1, bool begins,
-                   uint8_t* lds) {
+                   int tid, uint8_t* lds) {
   constexpr int kEights = D / 8, kAtOnce = 4;
   const int rows = min(16 * MT, A.rows - row0), items = rows * kEights, parts = w1 - w0 + 1;
   const int shares = max(1, kAttendThreads / items);
-  const int tid = threadIdx.x;
   f4* sums = (f4*)lds;                                    // [2][threads]
   f2* stats = (f2*)(lds + kAttendThreads * 32);
   for (int i0 = 0; i0 < items; i0 += kAttendThreads) {
@@ -379,10 +400,9 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   __shared__ __align__(16) uint8_t lds[kLds];
   float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
-  __shared__ int totals[3][4], found[4], list[2], shared_by[3], is_last;
+  __shared__ int totals[3][4], most_units[4], found[4], list[3], shared_by[3], is_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int j = lane & 15, h = lane >> 4;
   const int heads = A.a.cache.heads, per_unit = heads * A.row_tiles;
 
   // The requests' first units in the list, and the request of this workgroup's first one.
@@ -395,19 +415,20 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   // a workgroup the ends of two.  (8 requests of 8192 to 16384 positions 32.5 us, with even
   // shares 33.4; windows of 1024 positions, 32 requests of 16 heads in fp32, 16.8 and 17.8.)
   int most = 0, mine = 0, start = 0;
+  bool solo = false;
 #pragma nounroll
   for (int i = 0; i < 3; ++i) {
     const int m = i == 0 ? 1 : i == 1 ? even : even + 1 + even / 16;
-    int own = tid * each < A.a.B ? pieces_of(lane_first.units, m) * per_unit : 0;
+    int own = tid * each < A.a.B ? pieces_of(lane_first.units, m) * per_unit : 0, longest = lane_first.units;
     for (int k = 1; k < each; ++k)
-      if (tid * each + k < A.a.B) own += pieces_of(Range(A, tid * each + k).units, m) * per_unit;
-    int upto = own;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int below = __shfl_up(upto, d);
-      if (lane >= d) upto += below;
-    }
-    if (lane == 63) totals[i][wave] = upto;
+      if (tid * each + k < A.a.B) {
+        const int n = Range(A, tid * each + k).units;
+        own += pieces_of(n, m) * per_unit;
+        longest = max(longest, n);
+      }
+    const int upto = lanes_upto(own, [](int x, int y) { return x + y; });
+    longest = lanes_upto(longest, [](int x, int y) { return max(x, y); });
+    if (lane == 63) totals[i][wave] = upto, most_units[wave] = longest;
     __syncthreads();
     int ahead = upto - own;
     items = 0;
@@ -423,6 +444,15 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       // a part more of a run is as many bytes more for the one that joins them
       G = __builtin_amdgcn_readfirstlane(min((float)all * A.few < 1.f ? min(A.workgroups, kAttendFew) : A.workgroups, all));
       even = G > 0 ? over((double)all + G - 1, G) : 0;
+      // Many short runs: a wave does whole ones by itself, 4 steps of 32 positions a unit and
+      // some 4 for the rest, where a workgroup takes one step a unit and the time of 8 to
+      // load queries and tables and to join its waves.  (122 requests of 8 positions, 5 heads of
+      // 256 channels in 8 bits: 10.0 us, by workgroups 20.2; 256 of 100, 16 heads of 128 in
+      // 4 bits 23 and 33; but 90 of 700, 8 heads 26.1 and 20.4, and the rule takes workgroups.)
+      const int longest = max(max(most_units[0], most_units[1]), max(most_units[2], most_units[3]));
+      const float runs = (float)(A.a.B * per_unit), waves = 4.f * (float)A.workgroups;
+      solo = __builtin_amdgcn_readfirstlane(
+          all > G && ceilf(runs / waves) * (float)(longest + 1) * waves < (float)all + 8.f * runs);
     } else if (items > G) {
       continue;
     } else {
@@ -430,15 +460,19 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
     }
     mine = own;
     start = ahead;
-    if (even <= 1 || i > 0) break;
+    if (even <= 1 || solo || i > 0) break;
   }
   int u = 0, end = 0;
-  if (most == 0 && me < G) {
+  if (solo) {
+    const int slot = 4 * me + wave, runs = A.a.B * per_unit;
+    u = over((double)slot * runs, 4 * A.workgroups);
+    end = over((double)(slot + 1) * runs, 4 * A.workgroups);
+  } else if (most == 0 && me < G) {
     u = over((double)me * all, G);
     end = over((double)(me + 1) * all, G);
   }
   const int item = most > 0 ? me : u;
-  if (item >= start && item < start + mine) {
+  if (!solo && item >= start && item < start + mine) {
     Range r = lane_first;
     int b = tid * each;
     for (int n; item >= start + (n = pieces_of(r.units, max(most, 1)) * per_unit);) {
@@ -461,18 +495,33 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   } else if (tid == 0) {
     list[0] = all, list[1] = G;
   }
-  const bool alone = most > 0;
+  if (tid == 0) list[2] = most;
 
+  if (solo) b = -1;
   while (u < end) {
-    const int n = range.units;
-    if (u >= base + n * per_unit) {
-      base += n * per_unit;
-      range = Range(A, ++b);
-      continue;
+    const int lane = thread_again(wave) & 63, j = lane & 15, h = lane >> 4;
+    int run, from;
+    if (solo) {
+      const int at = over(u, per_unit);
+      if (at != b) range = Range(A, b = at);
+      run = u - b * per_unit;
+      from = 0;
+      if (range.units == 0) {
+        ++u;
+        continue;
+      }
+    } else {
+      if (u >= base + range.units * per_unit) {
+        base += range.units * per_unit;
+        range = Range(A, ++b);
+        continue;
+      }
+      run = over(u - base, range.units);
+      from = (u - base) - run * range.units;
     }
-    const int run = over(u - base, n), from = (u - base) - run * n, to = min(n, from + (end - u));
+    const int n = range.units, to = solo ? n : min(n, from + (end - u));
     const int head = run / A.row_tiles, row0 = (run - head * A.row_tiles) * (16 * MT);
-    u += to - from;
+    u += solo ? 1 : to - from;
 
     // the queries of this lane's rows, and the positions that these see
     u4 q[MT][kParts][kSteps];
@@ -701,13 +750,14 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
 
     // While 32 positions are used the next ones' codes are on their way to LDS, and the
     // table's entries of those behind them.
-    int p = (range.first + from) * kUnit + 32 * wave;
+    const int step = solo ? 32 : kUnit;
+    int p = solo ? range.lo & ~31 : (range.first + from) * kUnit + 32 * wave;
     const int p_end = min(range.hi, (range.first + to) * kUnit);
-    if (p + 32 <= range.lo) p += kUnit;
+    if (p + 32 <= range.lo) p += step;
     if (p < p_end) {
       uint32_t row = row_of(entry(p), p);
       C::load(A.a.cache, row == kNoRow ? 0 : row, own, lane);
-      int next = p + kUnit < p_end ? entry(p + kUnit) : -1;
+      int next = p + step < p_end ? entry(p + step) : -1;
       for (;;) {
         C c;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -716,13 +766,13 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
         c.take(own, j, h);
         const uint32_t there = (uint32_t)__ballot(row != kNoRow), used = row;
         const int at = p;
-        p += kUnit;
+        p += step;
         if (p < p_end) {
           // (what is read of it has arrived in registers before it is written again)
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           row = row_of(next, p);
           C::load(A.a.cache, row == kNoRow ? 0 : row, own, lane);
-          if (p + kUnit < p_end) next = entry(p + kUnit);
+          if (p + step < p_end) next = entry(p + step);
         }
         __builtin_amdgcn_s_setprio(0);
         use(c, at, used, there);
@@ -730,8 +780,34 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       }
     }
 
+    if (solo) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        uint32_t g = (uint32_t)(row0 + 16 * m + j);
+        if ((int)g >= A.rows) continue;
+        const int r = (int)A.by_group.split(g);
+        const bool fresh = r < range.fresh;
+        count<P::N>([&](auto pc) {
+          constexpr int w = P::width(pc), base_ch = P::base(pc), N = w / 16 < 4 ? w / 16 : 4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < w / 16; e += N) {
+              f4 o{0, 0, 0, 0};
+#pragma unroll
+              for (int x = 0; x < N; ++x) o[x] = acc[m][base_ch / 16 + e + x][i];
+              finish<DT, N>(A, b, r, head * A.group + (int)g, D, base_ch + (4 * h + i) * (w / 16) + e,
+                            fresh ? ref[m] : -INFINITY, fresh ? sum[m][0] : 0.f, o);
+            }
+        });
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      continue;
+    }
+
     // The four waves' parts of the run, and what becomes of them.
     const bool complete = from == 0 && to == n;
+    const int tid = thread_again(wave);
     const int slot = 2 * me + (from > 0 ? 0 : 1);       // (a run that an earlier workgroup began comes first)
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -778,7 +854,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
     // (a part is in memory before it is counted, whichever wave stored it)
     if (!complete) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (!alone && tid == 0) {
+      if (tid == 0 && list[2] == 0) {
         // the workgroups of its first and last unit: the last w with w all / G <= unit
         const int all = list[0], G = list[1], u0 = base + run * n, w0 = over((u0 + 1.) * G - 1, all);
         shared_by[0] = w0, shared_by[1] = over(((double)u0 + n) * G - 1, all), shared_by[2] = over((double)w0 * all, G) <= u0;
@@ -795,7 +871,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
         if (is_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
       __syncthreads();
-      if (is_last) join<DT, D, MT>(A, range, b, head, row0, shared_by[0], shared_by[1], shared_by[2], lds);
+      if (is_last) join<DT, D, MT>(A, range, b, head, row0, shared_by[0], shared_by[1], shared_by[2], tid, lds);
       __syncthreads();
     }
   }
@@ -803,7 +879,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   // rows of requests without a unit
   for (int b = me; b < A.a.B; b += (int)gridDim.x) {
     if (Range(A, b).units > 0) continue;
-    for (int i = tid; i < A.a.R * A.a.q_heads * (D / 4); i += kAttendThreads) {
+    for (int i = thread_again(wave); i < A.a.R * A.a.q_heads * (D / 4); i += kAttendThreads) {
       const int at = i / (D / 4);
       finish<DT>(A, b, at / A.a.q_heads, at % A.a.q_heads, D, (i - at * (D / 4)) * 4, -INFINITY, 0.f, f4{0, 0, 0, 0});
     }

@@ -408,6 +408,24 @@ def test_attend_shares(bits, dtype, units, window):
     check_attend(q, cache, table, lengths, bits, window=window)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("D,H,window", [(64, 8, 0), (96, 8, 70), (128, 48, 0), (192, 8, 33), (256, 8, 0)])
+def test_attend_many_short_requests(dtype, bits, D, H, window):
+    """More requests of a unit at most than there are workgroups, some without positions,
+    rows or blocks; with heads of 128 channels also twice as long."""
+    rng = np.random.default_rng(D + H)
+    B, R = 110, 3
+    lengths = rng.integers(0, 126, B)
+    lengths[:4] = 0, 1, 125, 31
+    new = rng.integers(0, R + 1, B)
+    new[:4] = R, R, R, 0
+    for at in (lengths, lengths + 90)[:1 if D != 128 else 2]:
+        q, cache, table = attend_inputs(rng, B, R, H, 8, D, bits, 24, dtype, at)
+        table[5, 0], table[6], table[7, -1] = -1, cache[0].shape[0], 2 ** 31 - 1
+        check_attend(q, cache, table, at, bits, new_tokens=new, window=window)
+
+
 def test_attend_many_requests():
     rng = np.random.default_rng(9)
     B = 700
