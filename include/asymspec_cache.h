@@ -154,9 +154,9 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
  *   window       0 or more
  *   workspace    >= asymspec_attend_workspace_size bytes, 16-byte aligned.  Its
  *                first ASYMSPEC_ATTEND_COUNTERS bytes are zero before its first use
- *                (for a single call the first 128 * B * heads * ceil(R * q_heads /
- *                heads / 16) of them are enough), and each call leaves them so for the
- *                next one, of any shape.  Calls that may run at the same time
+ *                (for a single call the first 128 * max(2048, B * heads * ceil(R *
+ *                q_heads / heads / 16)) of them are enough), and each call leaves them so
+ *                for the next one, of any shape.  Calls that may run at the same time
  *                (replays of captured ones among them) need distinct ones
  * The outputs and the workspace overlap no other array.  dim is 64, 96, 128, 192
  * or 256; 1 <= B <= 4096, 1 <= R <= 64; q_heads is a multiple of the cache's

@@ -43,6 +43,7 @@ namespace asym_cache {
 constexpr int kAttendThreads = 256;
 constexpr int kUnit = 128;                        // positions of a unit: 32 a wave
 constexpr int kAttendFew = 256;                   // workgroups: one a compute unit
+constexpr int kMostWorkgroups = 1024;             // four a compute unit at most
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 constexpr uint32_t kOnes = 0x3F803F80u;           // two bf16
 constexpr float kLog2E = 1.44269504088896340736f;
@@ -261,6 +262,14 @@ struct Codes {
   }
 };
 
+// The kernel's arguments where they lie, loaded as they are needed: held from its start, they
+// are more than the scalar registers, and spill.  (One row over 2048 positions 9.7 us, so 10.1.)
+STEP_DEV const AttendArgs& arguments() {
+  auto p = (const __attribute__((address_space(4))) AttendArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const AttendArgs*)p;
+}
+
 // The thread's number, from its wave's: neither it nor what is computed from it waits in
 // registers.
 STEP_DEV int thread_again(int wave) {
@@ -298,14 +307,23 @@ STEP_DEV void leave(float* p, float x, float y) {
 template <class T>
 STEP_DEV T left(const T* p) { return __builtin_nontemporal_load(p); }
 
-// Joins what workgroups w0 to w1 have of a run.  A thread has eight channels of a row,
-// and with few rows a share of the parts, of which it loads four at a time (more at once, or fewer,
-// take as long: what counts is that this code, which runs once, is short).
+// Which parts are joined, and where they are: a workgroup has two places, the second for a
+// run that it begins.  Of `parts` workgroups, `apart` from w0 on, the first one's part is in
+// its second place (`second`) and the others' in their first, or the other way about.  The
+// result is the rows' answer, or a part in place `to`.
+struct Join {
+  int w0, parts, apart, second, other, to;
+  STEP_DEV int place(int k) const { return 2 * (w0 + k * apart) + (k == 0 ? second : other); }
+};
+
+// Joins parts of a run.  A thread has eight channels of a row, and with few rows a share of
+// the parts, of which it loads four at a time (two at once take up to a quarter longer, eight up
+// to 2 us: this code runs once, and is fetched for it).
 template <int DT, int D, int MT>
-STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, int w0, int w1, bool begins,
-                   int tid, uint8_t* lds) {
+STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, const Join& J, int tid,
+                   uint8_t* lds) {
   constexpr int kEights = D / 8, kAtOnce = 4;
-  const int rows = min(16 * MT, A.rows - row0), items = rows * kEights, parts = w1 - w0 + 1;
+  const int rows = min(16 * MT, A.rows - row0), items = rows * kEights, parts = J.parts;
   const int shares = max(1, kAttendThreads / items);
   f4* sums = (f4*)lds;                                    // [2][threads]
   f2* stats = (f2*)(lds + kAttendThreads * 32);
@@ -320,8 +338,7 @@ STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int
       f2 st[kAtOnce];
       count<kAtOnce>([&](auto c) {
         const int k = min(k0 + c * shares, parts - 1);
-        // (a workgroup's second place is that of a run that it begins)
-        const int64_t at = (int64_t)(2 * (w0 + k) + (k == 0 && begins ? 1 : 0)) * (16 * MT) + row;
+        const int64_t at = (int64_t)J.place(k) * (16 * MT) + row;
         st[c] = left(A.stats + at);
         const f4* from = (const f4*)(A.sums + at * D + ch);
         x[c][0] = left(from);
@@ -368,7 +385,14 @@ STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int
         }
       }
     }
-    if (is && share == 0) {
+    if (is && share == 0 && J.to >= 0) {
+      const int64_t at = (int64_t)J.to * (16 * MT) + row;
+      for (int e = 0; e < 2; ++e) {
+        leave(A.sums + at * D + ch + 4 * e, o[e][0], o[e][1]);
+        leave(A.sums + at * D + ch + 4 * e + 2, o[e][2], o[e][3]);
+      }
+      if (ch == 0) leave((float*)&A.stats[at], top, total);
+    } else if (is && share == 0) {
       uint32_t g = (uint32_t)(row0 + row);
       const int r = (int)A.by_group.split(g);
       const bool fresh = r < range.fresh;
@@ -386,7 +410,8 @@ STEP_DEV int over(double a, int b) { return __builtin_amdgcn_readfirstlane((int)
 STEP_DEV int pieces_of(int units, int most) { return most == 1 ? units : (units + most - 1) / most; }
 
 template <int BITS, int DT, int D, int MT>
-__global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs A) {
+__global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_BF16, D, MT)) void attend_kernel(AttendArgs) {
+  const AttendArgs& A = arguments();
   typedef Pieces<D> P;
   typedef Codes<BITS, D> C;
   typedef typename Row<DT>::T T;
@@ -400,7 +425,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   __shared__ __align__(16) uint8_t lds[kLds];
   float (*buf)[16][kStride] = (float (*)[16][kStride])lds;
   __shared__ float2 stat[4][16];
-  __shared__ int totals[3][4], most_units[4], found[4], list[3], shared_by[3], is_last;
+  __shared__ int totals[3][4], most_units[4], found[4], list[3], shared_by[2], is_last;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int heads = A.a.cache.heads, per_unit = heads * A.row_tiles;
@@ -453,6 +478,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       const float runs = (float)(A.a.B * per_unit), waves = 4.f * (float)A.workgroups;
       solo = __builtin_amdgcn_readfirstlane(
           all > G && ceilf(runs / waves) * (float)(longest + 1) * waves < (float)all + 8.f * runs);
+      if (even == 1) most = 1;
     } else if (items > G) {
       continue;
     } else {
@@ -484,11 +510,11 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(found[0]), base = __builtin_amdgcn_readfirstlane(found[1]);
   Range range(A, __builtin_amdgcn_readfirstlane(found[2]), __builtin_amdgcn_readfirstlane(found[3]));
-  // (what a run's end needs waits in LDS: its workgroups, and whether its first one begins with it)
+  // (what a run's end needs waits in LDS)
   if (most > 0 && me < items) {
     const int n = range.units, pieces = __builtin_amdgcn_readfirstlane(pieces_of(n, most));
     const int run = over(me - base, pieces), piece = (me - base) - run * pieces;
-    if (tid == 0) shared_by[0] = me - piece, shared_by[1] = me - piece + pieces - 1, shared_by[2] = 1;
+    if (tid == 0) shared_by[0] = me - piece, shared_by[1] = pieces;
     base = 0;                                             // (units of this request)
     u = run * n + over((double)n * piece, pieces);
     end = run * n + over((double)n * (piece + 1), pieces);
@@ -851,27 +877,60 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
         }
       }
     }
-    // (a part is in memory before it is counted, whichever wave stored it)
+    Join J{0, 1, 1, 1, 0, -1};
+    int counter = 0, w0 = 0, group = 0, groups = 1;
     if (!complete) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (tid == 0 && list[2] == 0) {
+      const int most = __builtin_amdgcn_readfirstlane(list[2]);
+      if (most > 0) {
+        w0 = __builtin_amdgcn_readfirstlane(shared_by[0]);
+        J.parts = __builtin_amdgcn_readfirstlane(shared_by[1]);
+        counter = w0;
+      } else {
         // the workgroups of its first and last unit: the last w with w all / G <= unit
-        const int all = list[0], G = list[1], u0 = base + run * n, w0 = over((u0 + 1.) * G - 1, all);
-        shared_by[0] = w0, shared_by[1] = over(((double)u0 + n) * G - 1, all), shared_by[2] = over((double)w0 * all, G) <= u0;
+        const int all = __builtin_amdgcn_readfirstlane(list[0]), G = __builtin_amdgcn_readfirstlane(list[1]);
+        const int u0 = base + run * n;
+        w0 = over((u0 + 1.) * G - 1, all);
+        J.parts = over(((double)u0 + n) * G - 1, all) - w0 + 1;
+        J.second = over((double)w0 * all, G) <= u0;
+        counter = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
       }
+      J.w0 = w0;
+      // Many parts are joined in groups first, each by the last to leave one of its own, and the
+      // last group to be joined joins the groups'.  A group's result is in the place that its
+      // first workgroup has left; that is one where each workgroup has one run.  (12 rows over
+      // 131072 positions of one head 21 us, at once 50; 4 rows over 8 heads 44.)
+      if (most > 0 && J.parts > 32) {
+        const int shares = max(1, kAttendThreads / (min(16 * MT, A.rows - row0) * (D / 8)));
+        if (J.parts > 8 + 24 * shares) {
+          group = __builtin_amdgcn_readfirstlane((int)sqrtf((float)J.parts));
+          const int first = over(me - w0, group) * group;
+          groups = over(J.parts + group - 1, group);
+          J = Join{w0 + first, min(group, J.parts - first), 1, first == 0, 0, 2 * (w0 + first) + (first != 0)};
+          counter = kMostWorkgroups + w0 + first;
+        }
+      }
+      // (a part is in memory before it is counted, whichever wave stored it)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     __syncthreads();                                      // (codes go there again)
     if (!complete) {
-      // (neighbours' counters lie in different lines: many workgroups count at once)
-      const int run_id = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
-      uint32_t* const done = A.done + ((run_id & 4095) * 32 + (run_id >> 12));
-      if (tid == 0) {
-        is_last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
-                  (uint32_t)(shared_by[1] - shared_by[0]);
-        if (is_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma nounroll
+      for (;;) {
+        if (tid == 0) {
+          // (neighbours' counters lie in different lines: many workgroups count at once)
+          uint32_t* const done = A.done + ((counter & 4095) * 32 + (counter >> 12));
+          is_last = __hip_atomic_fetch_add(done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(J.parts - 1);
+          if (is_last) __hip_atomic_store(done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!is_last) break;
+        join<DT, D, MT>(A, range, b, head, row0, J, tid, lds);
+        if (J.to < 0) break;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        J = Join{w0, groups, group, 0, 1, -1};
+        counter = w0;
       }
-      __syncthreads();
-      if (is_last) join<DT, D, MT>(A, range, b, head, row0, shared_by[0], shared_by[1], shared_by[2], tid, lds);
       __syncthreads();
     }
   }

@@ -236,7 +236,7 @@ PyObject* attend_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     out.make(dev);
     void* const stream = stream_of(a[9]);
     const size_t runs = (size_t)B * s.cache.heads * ((R * (H / s.cache.heads) + 15) / 16);
-    const size_t counters = std::min<size_t>(128 * runs, ASYMSPEC_ATTEND_COUNTERS);
+    const size_t counters = std::min<size_t>(128 * std::max<size_t>(runs, 2048), ASYMSPEC_ATTEND_COUNTERS);
     const Tensor ws = attend_workspace(bytes, counters, dev, stream);
     s.out = out.ptr<char>("out", 0, dev);
     if (with_lse) s.lse = out.ptr<float>("lse", 1, dev);

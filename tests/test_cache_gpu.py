@@ -408,6 +408,28 @@ def test_attend_shares(bits, dtype, units, window):
     check_attend(q, cache, table, lengths, bits, window=window)
 
 
+@pytest.mark.parametrize("bits,dtype,D,R,H,Hk,lengths", [
+    (4, "bf16", 128, 3, 4, 1, [4200]),              # 33 parts, 34 and 65 of 12 rows
+    (4, "bf16", 128, 3, 4, 1, [4300, 8200]),
+    (8, "bf16", 128, 3, 8, 1, [128 * 90 - 1]),      # two row tiles
+    (4, "fp32", 256, 1, 2, 2, [11000]),
+    (8, "bf16", 64, 5, 1, 1, [40000]),              # more units than workgroups
+    (4, "bf16", 96, 4, 2, 1, [36000, 0, 500])])
+def test_attend_joined_in_groups(bits, dtype, D, R, H, Hk, lengths):
+    """Few requests with so many parts that groups of them are joined first, with values
+    that are not numbers in some parts."""
+    rng = np.random.default_rng(D + R)
+    q, cache, table = attend_inputs(rng, len(lengths), R, H, Hk, D, bits, 32, dtype, lengths)
+    first, _ = check_attend(q, cache, table, lengths, bits)
+    for _ in range(3):
+        again = asp.attend_cache(q, on_gpu(cache), gpu(table), gpu(i32(lengths)))
+        assert torch.equal(again, first)
+    cache[3][table[0, 20], 0, 5, 1] = 255
+    check_attend(q, cache, table, lengths, bits)
+    cache[1][table[0, 40], 0, 7, 0] = 255
+    check_attend(q, cache, table, lengths, bits)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("bits", [4, 8])
 @pytest.mark.parametrize("D,H,window", [(64, 8, 0), (96, 8, 70), (128, 48, 0), (192, 8, 33), (256, 8, 0)])
