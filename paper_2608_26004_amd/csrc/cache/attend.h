@@ -7,8 +7,8 @@
 // runs are many and short, each wave takes whole runs by itself).  A wave
 // keeps a running reference and sum for each row, so that nothing is exchanged until the
 // units end; there the waves' parts meet in LDS, and parts of different workgroups in
-// memory, where the last one to leave its part joins them (in the workgroups' order,
-// whoever is last, so that the answer is always the same).
+// memory, where the last one to leave its part joins them, many of them in two steps (in the
+// workgroups' order, whoever is last, so that the answer is always the same).
 //
 // Both products run on 16x16x32 bf16 matrix instructions: a code times its scale is
 // exact in bf16.  For the scores a lane decodes what it loaded, with the order of the
@@ -24,7 +24,7 @@
 // alone take 267 and 79 us there, the arithmetic alone 200 and 70: decoding and the
 // exponentials keep the vector units 65% busy, the matrix ones 27%.  Where work is small the
 // ends weigh as much: 8 requests of 8192 to 16384 positions, 12 rows, 32.5 us, of it 5 the
-// waves' parts, 4 the join; one row over 2048 positions 10, of it 4 to 5 the join.
+// waves' parts, 4 the join; one row over 2048 positions 9.8, of it 4 to 5 the join.
 //
 // What was slower: codes loaded ahead in registers (they spill); two sets of 32 positions
 // in flight (104 us for 99 in the second case); eight waves a workgroup (301 for 295 in the first);

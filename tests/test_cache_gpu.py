@@ -585,6 +585,34 @@ def test_captured_steps_replay():
         assert all(torch.equal(a, b) for a, b in zip(s["cache"], mine)), i
 
 
+def test_captured_attend_replays_over_other_lengths():
+    """How a captured call shares its work is decided from the lengths of each replay; eager
+    calls with another workspace run in between."""
+    rng = np.random.default_rng(9)
+    B, most = 96, 8300
+    q, cache, table = attend_inputs(rng, B, 3, 32, 8, 128, 4, 32, "bf16", [most] + [300] * (B - 1))
+    q, c, t = q[:, :, :32], on_gpu(cache), gpu(table)
+    lengths = torch.zeros(B, dtype=torch.int32, device="cuda")
+    one = torch.tensor([most], dtype=torch.int32, device="cuda")
+
+    def body():
+        return (asp.attend_cache(q, c, t, lengths),
+                asp.attend_cache(q[:1, :, :4], tuple(x[:, :1].contiguous() for x in small), t[:1], one))
+    small = tuple(x[:, :1] for x in c)
+    body()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = body()
+    for n in ([300] * B, [most] + [0] * (B - 1), [most] + [300] * (B - 1), [20] * B, [0] * B, [most] + [1] * (B - 1)):
+        lengths.copy_(torch.tensor(n))
+        want = [x.clone() for x in body()]
+        g.replay()
+        asp.attend_cache(q[:2], c, t[:2], lengths[:2])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), n[:2]
+
+
 def test_two_streams():
     """Calls on two streams at once, each with a workspace of its own."""
     rng = np.random.default_rng(8)
