@@ -318,7 +318,7 @@ struct Join {
 
 // Joins parts of a run.  A thread has eight channels of a row, and with few rows a share of
 // the parts, of which it loads four at a time (two at once take up to a quarter longer, eight up
-// to 2 us: this code runs once, and is fetched for it).
+// to 2.5 us: this code runs once, and is fetched for it).
 template <int DT, int D, int MT>
 STEP_DEV void join(const AttendArgs& A, const Range& range, int b, int head, int row0, const Join& J, int tid,
                    uint8_t* lds) {
