@@ -51,7 +51,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 struct AttendArgs {
   asymspec_attend a;
-  uint32_t* done;       // workgroups that have left their part, of each run; zero between calls
+  uint32_t* done;       // parts that are left, of each run or group of its parts; zero between calls
   float* sums;          // [2 workgroups][16 MT][dim]: parts of runs
   f2* stats;            // [2 workgroups][16 MT]: reference, sum
   int group;            // query heads of a head of the cache

@@ -133,8 +133,8 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   // With all workgroups that fit, not one a compute unit, codes stream at 5.2 TB/s
   // instead of 4.5; a run's join grows by its parts' bytes, at some 40 a ns.  So the
   // latter where 3.2e-8 us a byte of codes is less than 2.4e-5 us a byte of parts.  (8
-  // requests of 16384 positions in 4 bits, two heads: 16 rows 25 us and 23, 32 rows 39
-  // and 32; with 8 heads, 12 rows 34 and 40.)
+  // requests of 16384 positions in 4 bits, two heads: 16 rows 26 us and 20, 32 rows 37
+  // and 28; with 8 heads, 12 rows 33 and 42.)
   const double codes = kUnit * 2.0 * (c.dim * c.bits / 8 + c.dim / kBlock);
   const double parts = (A->workgroups - kAttendFew) * 4.0 * std::min(16 * *tiles, A->rows) * c.dim / (double)(runs * A->row_tiles);
   A->few = parts > 0 ? (float)(codes / (750 * parts)) : 1e9f;
