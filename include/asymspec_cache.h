@@ -157,7 +157,9 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
  *                (for a single call the first 128 * max(2048, B * heads * ceil(R *
  *                q_heads / heads / 16)) of them are enough), and each call leaves them so
  *                for the next one, of any shape.  Calls that may run at the same time
- *                (replays of captured ones among them) need distinct ones
+ *                (replays of captured ones among them) need distinct ones.  (What
+ *                workgroups leave for each other lies on whole lines of 128 bytes in
+ *                it, wherever it begins: the size has room for that)
  * The outputs and the workspace overlap no other array.  dim is 64, 96, 128, 192
  * or 256; 1 <= B <= 4096, 1 <= R <= 64; q_heads is a multiple of the cache's
  * heads, at most 64 times as many; max_blocks >= 1, max_blocks * block_size below

@@ -44,6 +44,7 @@ constexpr int kAttendThreads = 256;
 constexpr int kUnit = 128;                        // positions of a unit: 32 a wave
 constexpr int kAttendFew = 256;                   // workgroups: one a compute unit
 constexpr int kMostWorkgroups = 1024;             // four a compute unit at most
+constexpr int kLine = 128;                        // bytes of a line of the caches
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 constexpr uint32_t kOnes = 0x3F803F80u;           // two bf16
 constexpr float kLog2E = 1.44269504088896340736f;
@@ -52,8 +53,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 struct AttendArgs {
   asymspec_attend a;
   uint32_t* done;       // parts that are left, of each run or group of its parts; zero between calls
-  float* sums;          // [2 workgroups][16 MT][dim]: parts of runs
-  f2* stats;            // [2 workgroups][16 MT]: reference, sum
+  float* sums;          // [2 workgroups][16 MT][dim]: parts of runs, from a line's beginning on
+  f2* stats;            // [2 workgroups][16 MT]: reference, sum; the same
   int group;            // query heads of a head of the cache
   int rows;             // R * group
   int row_tiles;        // of 16 MT rows
@@ -297,9 +298,13 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
 }
 
 // Two floats for another workgroup, which may be on another die: stored past both
-// caches.  Each place has lines of its own, which one workgroup stores and one loads in
-// a call, behind the counter, so that no cache holds them from before.  (An agent's
-// fences write back and drop a die's whole cache, which cost 100 us a call.)
+// caches.  Each place has lines of its own (the first begins on one, and they are whole
+// lines), which one workgroup stores and one loads in a call, behind the counter, so that
+// no cache holds them from before: a line that two places share would be in a die's cache
+// once one of them is joined there, and the other be read as it was then.  (The place that
+// a group's result goes to is loaded and stored by the one that joins the group, whose
+// stores pass through its own die's caches, and loaded by another behind a counter.)
+// (An agent's fences write back and drop a die's whole cache, which cost 100 us a call.)
 STEP_DEV void leave(float* p, float x, float y) {
   const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
   __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
@@ -419,6 +424,7 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   constexpr int kProb = DT == ASYMSPEC_BF16 ? 2 : 3;       // of a probability
   constexpr int kSteps = D / 32, kTiles = D / 16;          // matrix instructions along a head
   constexpr int kStride = D + 4;                           // of a row in LDS: 16 rows, all banks
+  static_assert(16 * MT * sizeof(f2) % kLine == 0 && 16 * MT * D * sizeof(float) % kLine == 0, "places are whole lines");
   // codes on their way, and at the end of a run the waves' sums
   constexpr int kJoinBytes = kAttendThreads * 40;
   constexpr int kSumBytes = 4 * 16 * kStride * 4 > kJoinBytes ? 4 * 16 * kStride * 4 : kJoinBytes, kLds = kSumBytes > 4 * C::kBytes ? kSumBytes : 4 * C::kBytes;

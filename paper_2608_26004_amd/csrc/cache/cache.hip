@@ -28,6 +28,7 @@ constexpr long long kMostTokens = (1ll << 31) - 16;
 constexpr int kMostHeads = 4096;
 constexpr int kUnits = 256;                       // compute units of the chip
 constexpr int kMostRuns = ASYMSPEC_ATTEND_COUNTERS / 4;
+constexpr size_t kWorkspaceAlign = 16;
 
 static int element(int dtype) { return dtype == ASYMSPEC_BF16 ? 2 : 4; }
 static bool typed(int dtype) { return dtype == ASYMSPEC_BF16 || dtype == ASYMSPEC_FP32; }
@@ -113,8 +114,14 @@ static long long move_parts(MoveArgs& M, int requests) {
   return tiles < (1ll << 24) && tiles * heads < (1ll << 24) ? tiles * groups : -1;
 }
 
-// Row tiles of 16 rows, and the workspace of an attention; 0 for invalid sizes.
-static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, size_t* stats_at, size_t* sums_at) {
+// Where the parts begin: behind the counters, on a line, as they need.
+static char* attend_parts(void* workspace) {
+  return (char*)(((uintptr_t)workspace + kMostRuns * 4 + kLine - 1) / kLine * kLine);
+}
+
+// Row tiles of 16 rows, and the workspace of an attention; 0 for invalid sizes.  sums_at: of
+// the sums, behind the parts' beginning.
+static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, size_t* sums_at) {
   const asymspec_cache& c = a.cache;
   if (!valid(c) || !typed(a.dtype)) return 0;
   if (c.dim != 64 && c.dim != 96 && c.dim != 128 && c.dim != 192 && c.dim != 256) return 0;
@@ -139,9 +146,8 @@ static size_t attend_sizes(const asymspec_attend& a, AttendArgs* A, int* tiles, 
   const double parts = (A->workgroups - kAttendFew) * 4.0 * std::min(16 * *tiles, A->rows) * c.dim / (double)(runs * A->row_tiles);
   A->few = parts > 0 ? (float)(codes / (750 * parts)) : 1e9f;
   const size_t slots = 2 * (size_t)A->workgroups * 16 * *tiles;
-  *stats_at = kMostRuns * 4;
-  *sums_at = *stats_at + slots * sizeof(f2);
-  return *sums_at + slots * c.dim * 4;
+  *sums_at = slots * sizeof(f2);
+  return kMostRuns * 4 + (kLine - kWorkspaceAlign) + *sums_at + slots * c.dim * 4;
 }
 
 }  // namespace asym_cache
@@ -297,8 +303,8 @@ size_t asymspec_attend_workspace_size(const asymspec_attend* attend) {
   if (attend == nullptr) return 0;
   AttendArgs A;
   int tiles;
-  size_t stats_at, sums_at;
-  return attend_sizes(*attend, &A, &tiles, &stats_at, &sums_at);
+  size_t sums_at;
+  return attend_sizes(*attend, &A, &tiles, &sums_at);
 }
 
 int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t workspace_bytes, void* stream) {
@@ -307,8 +313,8 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   A.a = *attend;
   asymspec_attend& a = A.a;
   int tiles;
-  size_t stats_at, sums_at;
-  const size_t bytes = attend_sizes(a, &A, &tiles, &stats_at, &sums_at);
+  size_t sums_at;
+  const size_t bytes = attend_sizes(a, &A, &tiles, &sums_at);
   if (bytes == 0) return ASYMSPEC_E_ARG;
   if (a.q.at == nullptr || a.out == nullptr || a.block_table == nullptr || a.lengths == nullptr || workspace == nullptr)
     return ASYMSPEC_E_ARG;
@@ -317,7 +323,7 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   if (rc != ASYMSPEC_OK) return rc;
   const int el = element(a.dtype);
   if (!aligned(a.q.at, el) || !aligned(a.out, 16) || !aligned(a.lse, 4) || !aligned(a.block_table, 4) ||
-      !aligned(a.lengths, 4) || !aligned(a.new_tokens, 4) || !aligned(workspace, 16))
+      !aligned(a.lengths, 4) || !aligned(a.new_tokens, 4) || !aligned(workspace, kWorkspaceAlign))
     return ASYMSPEC_E_ALIGN;
   if (workspace_bytes < bytes) return ASYMSPEC_E_WORKSPACE;
   const size_t rows = (size_t)a.B * a.R * a.q_heads, b4 = (size_t)a.B * 4;
@@ -329,8 +335,8 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   if (asym_step::overlap(s, 3, 11)) return ASYMSPEC_E_ARG;
   if (device_cus() == 0) return ASYMSPEC_E_DEVICE;
   A.done = (uint32_t*)workspace;
-  A.stats = (f2*)((char*)workspace + stats_at);
-  A.sums = (float*)((char*)workspace + sums_at);
+  A.stats = (f2*)attend_parts(workspace);
+  A.sums = (float*)(attend_parts(workspace) + sums_at);
   // (a scale of 0 is far below what a score's exponent shows)
   A.c = std::max(std::fabs(a.scale) * kLog2E, 1e-30f);
   A.flip = std::signbit(a.scale) ? (a.dtype == ASYMSPEC_BF16 ? 0x80008000u : 0x80000000u) : 0;

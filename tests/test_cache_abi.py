@@ -270,6 +270,17 @@ def test_attend_workspace_size():
         assert size(**bad) == 0
 
 
+def test_attend_workspace_has_room_for_whole_lines():
+    """Workgroups' parts are read through caches whose lines hold 128 bytes, and must share none.
+    They begin on a line, wherever a workspace begins (at a multiple of 16): 112 bytes ahead
+    of them at most, and nothing but whole lines otherwise."""
+    def size(c=None, **over):
+        return library().asymspec_attend_workspace_size(ctypes.byref(attend(c, **over)))
+    for c in (dict(), dict(dim=96, bits=8), dict(dim=128), dict(dim=192, bits=8), dict(dim=256)):
+        for over in (dict(), dict(B=1, R=1, max_blocks=1), dict(R=64), dict(dtype=asp.FP32, max_blocks=1000)):
+            assert size(c, **over) > 524288 + 112 and (size(c, **over) - 524288 - 112) % 128 == 0
+
+
 def test_null_structures_are_refused():
     lib = library()
     assert lib.asymspec_rotate_heads(None, None) == asp.E_ARG

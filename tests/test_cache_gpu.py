@@ -668,6 +668,42 @@ def test_one_workspace_for_calls_of_any_shape():
             assert not ws[:counters].any()
 
 
+@pytest.mark.parametrize("offset", [16, 64, 112])
+def test_a_workspace_that_begins_within_a_line(offset):
+    """A workspace of exactly the size asked for, at any multiple of 16 bytes: the same answers,
+    counters left zero, and nothing written beside it."""
+    import ctypes
+
+    import test_cache_abi as abi
+    lib = abi.library()
+    rng = np.random.default_rng(17)
+    counters = 524288
+    # even shares that cross runs, pieces of runs, joins in groups
+    for B, R, H, Hk, D, bits, S, lengths in ((40, 2, 8, 8, 128, 8, 32, [383, 254] * 20), (3, 3, 8, 2, 64, 4, 16, [4000, 0, 900]),
+                                             (1, 3, 4, 1, 128, 4, 32, [8200])):
+        q, cache, table = attend_inputs(rng, B, R, H, Hk, D, bits, S, "fp32", lengths, garbage=False)
+        q = q.contiguous()
+        c, t, n = on_gpu(cache), gpu(table), gpu(i32(lengths))
+        want = asp.attend_cache(q, c, t, n, return_lse=True)
+        out, lse = (torch.full_like(x, 7) for x in want)
+        a = abi.Attend(cache=abi.Cache(*(x.data_ptr() for x in c), c[0].shape[0], Hk, S, D, bits),
+                       q=abi.Heads(q.data_ptr(), *q.stride()[:3]), out=out.data_ptr(), lse=lse.data_ptr(),
+                       block_table=t.data_ptr(), lengths=n.data_ptr(), new_tokens=None, scale=D ** -0.5, window=0, dtype=1,
+                       B=B, R=R, q_heads=H, max_blocks=t.shape[1])
+        size = lib.asymspec_attend_workspace_size(ctypes.byref(a))
+        memory = torch.full((size + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+        assert memory.data_ptr() % 512 == 0
+        memory[offset:offset + counters] = 0
+        for _ in range(3):
+            out.fill_(7)
+            st = torch.cuda.current_stream().cuda_stream
+            assert lib.asymspec_attend_cache(ctypes.byref(a), memory.data_ptr() + offset, size, st) == 0
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+            assert not memory[offset:offset + counters].any()
+            assert (memory[:offset] == 0x5A).all() and (memory[offset + size:] == 0x5A).all()
+
+
 def test_a_growing_workspace():
     """A call that needs a larger workspace while calls in the smaller one are still on
     their way, on a stream of its own."""
