@@ -55,7 +55,8 @@ def rotary_frequencies(channels: int, base: float = 10000.0, stretch: float = 1.
                 slowest pair is over `stretch`, the fastest stays
       "ramp"    pairs that turn `fast` times and more in `context` positions stay,
                 those that turn `slow` times and less are over `stretch`, and between
-                them the share that stays grows evenly with the pair's index
+                them the share that stays falls evenly with the pair's index (from
+                index 0 on at least, and to index channels - 1 at most)
     A ramp goes with rotate_heads' magnitude = 0.1 * log(stretch) + 1."""
     if channels < 2 or channels % 2:
         raise ValueError(f"channels must be even and at least 2, got {channels}")
@@ -69,13 +70,13 @@ def rotary_frequencies(channels: int, base: float = 10000.0, stretch: float = 1.
     elif kind == "linear":
         f = base ** (-2 * i / channels) / stretch
     elif kind == "ramp":
-        if not fast > slow > 0:
-            raise ValueError("fast must be above slow, and slow above 0")
+        if not (fast > slow > 0 and context > 0):
+            raise ValueError("fast must be above slow, and slow and context above 0")
         f = base ** (-2 * i / channels)
-        # the index of a pair that turns so often in the context
+        # the index of a pair that turns so often in the context, also where there is none
         at = [channels * math.log(context / (2 * math.pi * turns)) / (2 * math.log(base)) for turns in (fast, slow)]
-        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), channels // 2 - 1)
-        stay = 1 - ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), channels - 1)
+        stay = (1 - ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)) * (i < at[1])
         f = f * stay + f / stretch * (1 - stay)
     else:
         raise ValueError(f'kind must be "linear", "base" or "ramp", got {kind!r}')

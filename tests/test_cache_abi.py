@@ -456,3 +456,29 @@ def test_rotary_frequencies():
                 dict(channels=2, kind="base"), dict(kind="ramp", fast=1.0, slow=1.0)):
         with pytest.raises(ValueError):
             asp.rotary_frequencies(**{**dict(channels=64, device="cpu"), **bad})
+
+
+@pytest.mark.parametrize("channels,base,stretch,context,fast,slow", [
+    (128, 10000.0, 4.0, 65536, 32.0, 1.0), (128, 10000.0, 4.0, 131072, 32.0, 1.0), (128, 10000.0, 32.0, 1 << 20, 32.0, 1.0),
+    (64, 10000.0, 8.0, 4096, 32.0, 1.0), (64, 500.0, 8.0, 1 << 22, 32.0, 1.0), (96, 10000.0, 4.0, 100, 32.0, 1.0),
+    (128, 10000.0, 4.0, 6, 32.0, 1.0), (128, 10000.0, 4.0, 1, 32.0, 1.0), (32, 1000.0, 2.0, 4096, 1.001, 1.0)])
+def test_a_ramp_of_any_context(channels, base, stretch, context, fast, slow):
+    """Pairs that turn `fast` times and more stay, those that turn `slow` times and less are
+    stretched, and the share falls by the same from index to index in between: also where the
+    slowest pair still turns more than `slow` times, or none does so often."""
+    f = [base ** (-2 * i / channels) for i in range(channels // 2)]
+    got = asp.rotary_frequencies(channels, base=base, stretch=stretch, kind="ramp", context=context, fast=fast, slow=slow,
+                                 device="cpu").tolist()
+    turns = [x * context / (2 * math.pi) for x in f]
+    # the ramp's ends as whole indices, of pairs that there need not be
+    ratio = base ** (2 / channels)
+    lo = max(0, math.floor(math.log(turns[0] / fast) / math.log(ratio)))
+    hi = min(channels - 1, math.ceil(math.log(turns[0] / slow) / math.log(ratio)))
+    for i, (x, y, t) in enumerate(zip(f, got, turns)):
+        share = 0.0 if t <= slow else 1.0 if i <= lo else (hi - i) / (hi - lo)
+        want = x * share + x / stretch * (1 - share)
+        # a quotient, a difference, two products and a sum: 8 roundings of 2^-53, and the power's
+        assert abs(y - want) <= 16 * 2.0 ** -53 * x, (i, y, want)
+    for i, t in enumerate(turns):
+        assert got[i] == f[i] or abs(got[i] - f[i]) <= 4 * 2.0 ** -53 * f[i] or t < fast
+        assert abs(got[i] - f[i] / stretch) <= 4 * 2.0 ** -53 * f[i] or t > slow
