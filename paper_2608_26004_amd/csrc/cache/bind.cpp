@@ -152,8 +152,8 @@ PyObject* read_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::ScalarType st = type == ASYMSPEC_BF16 ? at::kBFloat16 : at::kFloat;
     if (B < 1 || top < 1 || H < 1) check(ASYMSPEC_E_ARG);
     // (ahead of the outputs' allocation)
-    const int64_t tile = 2048 / D;
-    if (B * ((W + tile - 1) / tile) >= (1ll << 24) / H) check(ASYMSPEC_E_ARG);
+    const int64_t tile = 2048 / D, tiles = B * ((W + tile - 1) / tile);
+    if (tiles >= 1ll << 24 || tiles * H >= 1ll << 24) check(ASYMSPEC_E_ARG);
     Outs out(a[6], 2);
     out.is(st, {B, W, H, D});
     out.is(st, {B, W, H, D});

@@ -425,6 +425,25 @@ def test_gradients_and_lazy_tensors_are_refused():
         asp.attend_cache(x, c, i(1, 1), i(1))
 
 
+@no_gpu
+@pytest.mark.parametrize("heads,dim", [(1, 32), (3, 64), (5, 256), (7, 96), (4096, 128)])
+def test_read_limit_is_the_documented_one(heads, dim):
+    """requests * ceil(width / floor(2048 / dim)) * heads below 2^24, also for heads that do not
+    divide 2^24.  (Tensors on the CPU, which are refused behind the check.)"""
+    c = asp.new_cache(1, heads, 1, dim, 8, device="cpu")
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)     # noqa: E731
+    for B in (1, 3):
+        tiles = ((1 << 24) - 1) // heads // B
+        width = tiles * (2048 // dim)
+        with pytest.raises(ValueError, match="must be on the GPU"):
+            asp.read_cache(c, i(B, 1), i(B), width)
+        with pytest.raises(asp.AsymSpecError) as e:
+            asp.read_cache(c, i(B, 1), i(B), width + 1)
+        assert e.value.status == asp.E_ARG
+    with pytest.raises(asp.AsymSpecError):
+        asp.read_cache(c, i(B, 1), i(B), 2 ** 31 - 1)
+
+
 # ------------------------------------------------------------------ helpers --
 def test_new_cache():
     c = asp.new_cache(3, 2, 5, 96, 4, device="cpu")
