@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 
 #include "../step/launch.h"
 #include "../step/span.h"
@@ -337,8 +338,13 @@ int asymspec_attend_cache(const asymspec_attend* attend, void* workspace, size_t
   A.done = (uint32_t*)workspace;
   A.stats = (f2*)attend_parts(workspace);
   A.sums = (float*)(attend_parts(workspace) + sums_at);
-  // (a scale of 0 is far below what a score's exponent shows)
-  A.c = std::max(std::fabs(a.scale) * kLog2E, 1e-30f);
+  // (what a row does not see has a score of -infinity, of which 0 times is no number: a scale
+  // of 0 is the smallest number there is, 2^-149, and takes scores up to 2^128 below 2^-21)
+  A.c = std::fabs(a.scale) * kLog2E;
+  uint32_t bits;
+  std::memcpy(&bits, &A.c, sizeof(bits));
+  if (bits == 0) bits = 1;
+  std::memcpy(&A.c, &bits, sizeof(bits));
   A.flip = std::signbit(a.scale) ? (a.dtype == ASYMSPEC_BF16 ? 0x80008000u : 0x80000000u) : 0;
   A.by_size = Div((uint32_t)a.cache.block_size);
   A.by_group = Div((uint32_t)A.group);

@@ -383,6 +383,20 @@ def test_attend_extremes():
     check_attend(q * 0, cache, table, lengths, 4)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-33, -3e-34, 2e-36])
+def test_attend_tiny_scales(dtype, scale):
+    """Scales far below 1, zero among them, of products far above it."""
+    rng = np.random.default_rng(18)
+    lengths = [200, 3]
+    q, cache, table = attend_inputs(rng, 2, 2, 4, 2, 64, 8, 16, dtype, lengths)
+    for part in (1, 3):
+        cache[part] = np.clip(cache[part], 120, 130)       # (garbage that is not seen, within fp32)
+    cache[1] += 53                                         # 2^53: products of some 1e34
+    check_attend((q.float() * 2.0 ** 58).to(q.dtype), cache, table, lengths, 8, scale=scale)
+    check_attend(q, cache, table, lengths, 8, scale=scale)
+
+
 @pytest.mark.parametrize("bits,S", [(4, 16), (8, 64), (4, 24)])
 def test_attend_long(bits, S):
     """Requests of very different lengths, cut over many workgroups."""
