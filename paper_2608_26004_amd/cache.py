@@ -150,6 +150,8 @@ def attend_cache(q, cache, block_table, lengths, new_tokens=None, scale=None, wi
     new_tokens[b] on are 0, their lse -inf.  What a row does not see has no effect on it,
     whatever is there.  out: the tensor, or with return_lse the two, to write, which
     overlap no other tensor of the call.  The workspace is memory kept for the calls of
-    each stream; a captured call has its own, in its graph's memory."""
+    each stream, and on hipStreamPerThread of each thread; a captured call has its own, in
+    its graph's memory.  A stream of other making (torch.cuda.ExternalStream) is not to be
+    destroyed before its calls have ended: its handle may come back as another stream's."""
     return (_s._step or _s._bind()).attend_cache(q, cache, block_table, lengths, new_tokens, scale, window, return_lse,
                                                  out, _s._stream(q))

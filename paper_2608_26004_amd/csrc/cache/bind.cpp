@@ -5,9 +5,10 @@
 #include "../step/binding.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <map>
-#include <utility>
+#include <tuple>
 
 #include "asymspec_cache.h"
 
@@ -182,10 +183,19 @@ Tensor attend_workspace(size_t bytes, size_t counters, const at::Device& dev, vo
     t.narrow(0, 0, (int64_t)counters).zero_();
     return t;
   }
+  // hipStreamPerThread is one handle for a stream of each host thread, to which the number
+  // of the thread belongs.
+  static std::atomic<uint64_t> threads{0};
+  static thread_local const uint64_t this_thread = ++threads;
+  const uint64_t thread = (hipStream_t)stream == hipStreamPerThread ? this_thread : 0;
   // (never destroyed: torch's allocator may be gone before this)
-  static auto& kept = *new std::map<std::pair<int, void*>, Tensor>;
-  Tensor& t = kept[{dev.index(), stream}];
+  static auto& kept = *new std::map<std::tuple<int, void*, uint64_t>, Tensor>;
+  Tensor& t = kept[{dev.index(), stream, thread}];
   if (!t.defined() || (size_t)t.numel() < bytes) {
+    // (torch gives memory that is freed to the next call on the same handle, which may be
+    // another thread's while this one's are under way.  So it stays; each is a quarter larger
+    // than the one before)
+    if (thread != 0 && t.defined()) new Tensor(t);
     t = Tensor();
     t = at::empty({(int64_t)(bytes + bytes / 4)}, as_bytes);
     t.narrow(0, 0, ASYMSPEC_ATTEND_COUNTERS).zero_();

@@ -735,6 +735,53 @@ def test_a_growing_workspace():
         assert torch.equal(g, want[i == 30]), i
 
 
+def test_threads_on_the_per_thread_stream():
+    """hipStreamPerThread is one handle, and another stream in each thread: each thread's calls
+    have a workspace of their own, the same one again, and keep it when they need a larger."""
+    import threading
+    rng = np.random.default_rng(19)
+    lengths = [3000, 100, 2000]
+    q, cache, table = attend_inputs(rng, 3, 2, 8, 2, 128, 4, 16, "bf16", lengths, garbage=False)
+    c, t, n = on_gpu(cache), gpu(table), gpu(i32(lengths))
+    want = asp.attend_cache(q, c, t, n, return_lse=True)
+    # (each thread's outputs are its own from the start: torch's allocator knows the handle alone)
+    outs = [[tuple(torch.full_like(x, 7) for x in want) for _ in range(8)] for _ in range(2)]
+    small = asp.attend_cache(q[:, :, ::4, :64].contiguous(), *(few := (asp.new_cache(1, 2, 16, 64), t[:, :1].contiguous(), n)))
+    small_outs = [torch.full_like(small, 7) for _ in range(2)]
+    qs = q[:, :, ::4, :64].contiguous()
+    torch.cuda.synchronize()
+    grown, ready = [], threading.Barrier(2)
+    taken = []
+
+    def work(me):
+        with torch.cuda.stream(torch.cuda.ExternalStream(2)):
+            for turn in range(2):                          # one thread after the other
+                if turn == me:
+                    before = torch.cuda.memory_allocated()
+                    asp.attend_cache(qs, *few, out=small_outs[me])
+                    taken.append(torch.cuda.memory_allocated() - before)
+                    asp.attend_cache(q, c, t, n, return_lse=True, out=outs[me][0])
+                    grown.append(torch.cuda.memory_allocated() - before)
+                    asp.attend_cache(q, c, t, n, return_lse=True, out=outs[me][1])
+                    grown.append(torch.cuda.memory_allocated() - before)
+                    torch.cuda.synchronize()
+                ready.wait(60)
+            for o in outs[me][2:]:                         # both at once
+                asp.attend_cache(q, c, t, n, return_lse=True, out=o)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    torch.cuda.synchronize()
+    assert len(grown) == 4 and taken[0] > 524288 and taken[1] == taken[0]
+    assert grown[0] > taken[0] and grown == grown[:1] * 4
+    assert all(torch.equal(a, b) for each in outs for o in each for a, b in zip(o, want))
+    assert all(torch.equal(x, small) for x in small_outs)
+
+
 def test_attend_most_requests():
     """4096 requests of one position, some of none, and rows of all of them."""
     rng = np.random.default_rng(14)
