@@ -28,8 +28,9 @@ FLAGS = [
 def units():
     """(object name, source, defines) of every object of the library: the host
     side, the operators around the decision step and those of the cache, the
-    attention's kernels per width of codes and type of queries, the cross-family kernels per storage type, and one object per instance of the
-    decision kernel (storage type x source of delta x variant), compiled in parallel."""
+    attention's kernels per width of codes and type of queries, the cross-family
+    kernels per storage type, and one object per instance of the decision kernel
+    (storage type x source of delta x variant), compiled in parallel."""
     out = [("asymspec", "asymspec.hip", []), ("step", os.path.join("step", "step.hip"), []),
            ("cache", os.path.join("cache", "cache.hip"), [])]
     for bits in (4, 8):

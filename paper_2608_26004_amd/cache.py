@@ -111,7 +111,8 @@ def write_cache(k, v, slots, cache):
     at most once).  For each 32 channels the scale is the smallest power of two (2^-100 at
     least) with which the largest magnitude is at most 448 (8 bits) or 6 (4 bits); each
     code is the nearest, ties to even.  Where one of the 32 is not finite (or beyond
-    1.5 * 2^127), all of them read as not a number.  Returns the cache, changed in place."""
+    1.75 * 2^127 with 8 bits, 1.5 * 2^127 with 4), all of them read as not a number.  Returns
+    the cache, changed in place."""
     return (_s._step or _s._bind()).write_cache(k, v, slots, cache, _s._stream(k))
 
 

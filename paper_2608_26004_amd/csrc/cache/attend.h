@@ -892,12 +892,12 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
         J.parts = __builtin_amdgcn_readfirstlane(shared_by[1]);
         counter = w0;
       } else {
-        // the workgroups of its first and last unit: the last w with w all / G <= unit
+        // the workgroups of its first and last unit: the last w with w all / G <= unit (so the
+        // first one begins the run, and has its part in its second place)
         const int all = __builtin_amdgcn_readfirstlane(list[0]), G = __builtin_amdgcn_readfirstlane(list[1]);
         const int u0 = base + run * n;
         w0 = over((u0 + 1.) * G - 1, all);
         J.parts = over(((double)u0 + n) * G - 1, all) - w0 + 1;
-        J.second = over((double)w0 * all, G) <= u0;
         counter = (b * heads + head) * A.row_tiles + row0 / (16 * MT);
       }
       J.w0 = w0;

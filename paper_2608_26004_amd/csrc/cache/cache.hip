@@ -20,7 +20,6 @@ namespace asym_cache {
 
 using asym_step::aligned;
 using asym_step::device_cus;
-using asym_step::fits;
 using asym_step::launch;
 using asym_step::Span;
 
