@@ -91,6 +91,38 @@ def test_rotate(dtype, B, R, H, Hk, D, n, interleaved):
     assert torch.equal(alone, got[0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("B,R,H,Hk,D,n", [
+    (10003, 1, 32, 8, 128, 64),             # more than the caches hold, one token a workgroup
+    (3335, 3, 31, 9, 128, 16),              # the same, four tokens, and one left over
+    (10003, 1, 5, 3, 64, 8),                # eight tokens a workgroup, three left over
+    (5001, 1, 3, 1, 32, 2),                 # eight, a pair at a time
+    (2051, 1, 6, 2, 128, 32)])              # two, one left over
+def test_rotate_many_tokens(dtype, interleaved, B, R, H, Hk, D, n):
+    """Calls of many tokens are those of few: against the same call in parts of 500 requests,
+    bit for bit, and some tokens against 64 bits."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(B + n)
+    qkv = (2 * torch.randn((B, R, H + 2 * Hk, D), device="cuda", generator=g)).to(DT[dtype])
+    q, k = qkv[:, :, :H], qkv[:, :, H:H + Hk]
+    pos = torch.randint(-100, 100000, (B,), device="cuda", generator=g).int()
+    f = gpu(10000.0 ** (-np.arange(n) / n))
+    kw = dict(interleaved=interleaved, magnitude=0.75)
+    got = asp.rotate_heads(q, k, pos, f, **kw)
+    for lo in range(0, B, 500):
+        part = asp.rotate_heads(q[lo:lo + 500], k[lo:lo + 500], pos[lo:lo + 500], f, **kw)
+        assert all(torch.equal(a[lo:lo + 500], b) for a, b in zip(got, part)), lo
+    some = torch.tensor([0, 1, 2, 3, 4, 5, 6, 7, B // 2, B - 4, B - 3, B - 2, B - 1], device="cuda")
+    p = pos[some].cpu().numpy()[:, None].astype(np.int64) + np.arange(R)
+    for x, y in zip((q, k), got):
+        want, err = rotated(f64(x[some]), p, f.cpu().numpy(), interleaved, 0.75)
+        assert (np.abs(f64(y[some]) - want) <= err + HALF[dtype] * np.abs(want) + TINY[dtype]).all()
+    rest = qkv[:, :, H + Hk:].clone()
+    asp.rotate_heads(q, k, pos, f, out=(q, k), **kw)       # in place
+    assert torch.equal(q, got[0]) and torch.equal(k, got[1]) and torch.equal(qkv[:, :, H + Hk:], rest)
+
+
 def test_rotate_heads_major_and_other_outputs():
     """Heads outside rows, requests in no order of memory, and outputs of other strides."""
     rng = np.random.default_rng(5)
@@ -163,6 +195,47 @@ def test_write(dtype, bits, tokens, heads, D, S):
     assert asp.write_cache(k, v, gpu(slots), cache) is cache
     ref.write(want, f64(k), f64(v), slots, bits)
     assert_cache(cache, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("tokens,R,heads,D", [(8200, 1, 5, 128), (2750, 3, 3, 256), (12000, 1, 7, 96)])
+def test_write_two_heads_a_lane(dtype, bits, tokens, R, heads, D):
+    """As many tokens as let a lane have two heads, the last one of an odd number alone."""
+    rng = np.random.default_rng(tokens)
+    S = 16
+    N = tokens * R // S + 5
+    want = empty(N, heads, S, D, bits, rng=rng)
+    cache = on_gpu(want)
+    slots = rng.permutation(N * S)[:tokens * R].astype(np.int64)
+    slots[rng.random(tokens * R) < 0.1] = -1
+    kv = stored(rng, (tokens, R, 2 * heads, D), dtype, 3.0)
+    k, v = kv[:, :, :heads], kv[:, :, heads:]
+    asp.write_cache(k, v, gpu(slots.reshape(tokens, R)), cache)
+    ref.write(want, f64(k).reshape(-1, heads, D), f64(v).reshape(-1, heads, D), slots, bits)
+    assert_cache(cache, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("heads,D", [(5, 128), (1, 256), (3, 160)])
+def test_write_more_than_the_caches_hold(dtype, bits, heads, D):
+    """Inputs above 96 MiB: against the same tokens in calls of 1000, bit for bit."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(heads + D)
+    tokens, S = (100 << 20) // (2 * heads * D * (2 if dtype == "bf16" else 4)), 32
+    N = tokens // S + 3
+    kv = (torch.randn((tokens, 2 * heads, D), device="cuda", generator=g) * 3).to(DT[dtype])
+    k, v = kv[:, :heads], kv[:, heads:]
+    slots = torch.randperm(N * S, device="cuda", generator=g)[:tokens]
+    slots[torch.rand(tokens, device="cuda", generator=g) < 0.1] = N * S
+    start = [torch.randint(0, 256, x.shape, device="cuda", generator=g, dtype=torch.uint8)
+             for x in asp.new_cache(N, heads, S, D, bits)]
+    got, want = (tuple(x.clone() for x in start) for _ in range(2))
+    asp.write_cache(k, v, slots, got)
+    for lo in range(0, tokens, 1000):
+        asp.write_cache(k[lo:lo + 1000], v[lo:lo + 1000], slots[lo:lo + 1000], want)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 @pytest.mark.parametrize("bits", [4, 8])
@@ -252,6 +325,26 @@ def test_read(dtype, bits, B, heads, D, S, L):
     o = (torch.empty_like(k), torch.empty_like(v))
     assert asp.read_cache(got_cache, gpu(table), gpu(lengths), L + 3, first=gpu(first), dtype=DT[dtype], out=o)[0] is o[0]
     assert all(torch.equal(a.nan_to_num(7), b.nan_to_num(7)) for a, b in zip(o, (k, v)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("B,heads,D,S,L", [(2, 5, 128, 16, 4200), (3, 3, 256, 24, 1900), (1, 7, 96, 7, 6300)])
+def test_read_two_heads_a_lane(dtype, bits, B, heads, D, S, L):
+    """As many positions as let a lane have two heads, the last one of an odd number alone."""
+    rng = np.random.default_rng(B + D)
+    N = B * (L // S + 2) + 4
+    cache = empty(N, heads, S, D, bits, rng=rng)
+    for p in (1, 3):
+        cache[p] = np.where(rng.random(cache[p].shape) < 0.02, 255, rng.integers(100, 150, cache[p].shape)).astype(np.uint8)
+    lengths = i32([L] + [L - 700] * (B - 1))
+    table = tables(rng, lengths, S, N)
+    table[0, 2] = -1
+    first = i32([17] * B)
+    for f in (None, first):
+        got = asp.read_cache(on_gpu(cache), gpu(table), gpu(lengths), L, first=gpu(f), dtype=DT[dtype])
+        for a, want in zip(got, ref.read(cache, table, lengths, L, f, bits)):
+            assert np.array_equal(f64(a), want, equal_nan=True)
 
 
 # ------------------------------------------------------------------- attend --
@@ -420,6 +513,35 @@ def test_attend_shares(bits, dtype, units, window):
     lengths = np.array([max(0, 128 * n - int(rng.choice([2, 3, 65]))) for n in units])
     q, cache, table = attend_inputs(rng, len(units), 2, 8, 8, 128, bits, 32, dtype, lengths)
     check_attend(q, cache, table, lengths, bits, window=window)
+
+
+@pytest.mark.parametrize("bits,dtype", [(4, "bf16"), (8, "bf16"), (4, "fp32"), (8, "fp32")])
+@pytest.mark.parametrize("shares", ["pieces", "larger pieces", "even"])
+def test_attend_shares_of_an_instance(bits, dtype, shares):
+    """The ways in which units are shared, for lengths that follow from the number of
+    workgroups of the instance (which its workspace's size shows)."""
+    import ctypes
+
+    import test_cache_abi as abi
+    heads, D, S, R = 8, 128, 32, 2
+    c = abi.Cache(None, None, None, None, 1 << 20, heads, S, D, bits)
+    a = abi.Attend(cache=c, q=abi.Heads(), scale=1.0, dtype=0 if dtype == "bf16" else 1, B=4096, R=R, q_heads=heads, max_blocks=100)
+    size = abi.library().asymspec_attend_workspace_size(ctypes.byref(a))
+    W, left = divmod(size - 524288 - 112, 2 * 16 * (8 + 4 * D))
+    assert left == 0 and W in (512, 768)
+    n = W // 32
+    units = {"pieces": [n] * 8, "larger pieces": [n - 1, n + 1] * 4, "even": [2, 3] * (W // 16 + 2)}[shares]
+    # what the kernel then finds: pieces of the even share's size, or one more, that are enough
+    # for all runs, or neither
+    everything = heads * sum(units)
+    even = -(-everything // W)
+    assert everything > W
+    taken = [heads * sum(-(-u // m) for u in units) <= W for m in (even, even + 1 + even // 16)]
+    assert taken == {"pieces": [True, True], "larger pieces": [False, True], "even": [False, False]}[shares]
+    rng = np.random.default_rng(n)
+    lengths = np.array([128 * u - int(rng.choice([2, 3, 65])) for u in units])
+    q, cache, table = attend_inputs(rng, len(units), R, heads, heads, D, bits, S, dtype, lengths)
+    check_attend(q, cache, table, lengths, bits)
 
 
 @pytest.mark.parametrize("bits,dtype,D,R,H,Hk,lengths", [
