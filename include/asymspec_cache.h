@@ -68,9 +68,9 @@ typedef struct asymspec_heads {
  * channels (i, i + n), or (2i, 2i + 1) where interleaved:
  *   x' = magnitude * (x cos(p f_i) - y sin(p f_i))
  *   y' = magnitude * (x sin(p f_i) + y cos(p f_i))
- * Angles are reduced in fp64, sines and cosines rounded to fp32, the products
- * and sums are fp32 and rounded once to the storage type.  Channels from 2n on
- * stay as they are.
+ * Angles are fp64; sines and cosines are fp32 numbers, two units off at most (small
+ * ones too); the products and sums are fp32 and rounded once to the storage type.
+ * Channels from 2n on stay as they are.
  *   q, k         [B][R][q_heads][dim] and [B][R][k_heads][dim] (dtype, aligned to
  *                an element); k_heads = 0: no k
  *   q_out, k_out the same shapes; each either its input with the same strides, or

@@ -42,13 +42,14 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(RotateArgs A) {
     uint32_t row = token;
     const uint32_t b = A.by_R.split(row);
     const long long p = r.every_row ? (long long)r.positions[token] : (long long)r.positions[b] + row;
-    // in turns: the whole ones leave in 64 bits, what stays is exact to 2^-24 of a turn
-    // and better
+    // in turns, of which the whole ones leave in 64 bits; of what stays the 24 bits that
+    // fp32 holds, and then the rest, below 2^-23 of a radian, to first order
     double t = (double)p * (r.frequencies[f] * 0.15915494309189533577);
     t -= rint(t);
+    const float near = (float)t, rest = (float)((t - (double)near) * 6.28318530717958647693);
     float s, c;
-    sincospif(2.0f * (float)t, &s, &c);
-    turn[i] = make_float2(c * r.magnitude, s * r.magnitude);
+    sincospif(2.0f * near, &s, &c);
+    turn[i] = make_float2(fmaf(-s, rest, c) * r.magnitude, fmaf(c, rest, s) * r.magnitude);
   }
   __syncthreads();
   const uint32_t heads = (uint32_t)(r.q_heads + r.k_heads);

@@ -91,6 +91,29 @@ def test_rotate(dtype, B, R, H, Hk, D, n, interleaved):
     assert torch.equal(alone, got[0])
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotate_sines_and_cosines(interleaved):
+    """The sine and cosine of an angle, as pairs (1, 0) show them in fp32: within 2 units each,
+    also where they are small, half a turn away from none and a quarter."""
+    rng = np.random.default_rng(20)
+    n, pos = 64, i32(rng.integers(0, 200000, 3000))
+    # any angles; and those p turns and a half or a quarter on, and a little, of which 64 bits
+    # hold all that counts
+    f = np.concatenate([10000.0 ** (-np.arange(n // 2) / (n // 2)),
+                        2 * math.pi * (np.array([0.5, 0.25] * (n // 4)) + 10.0 ** -rng.uniform(7, 12, n // 2))])
+    q = torch.zeros(len(pos), 1, 1, 2 * n, device="cuda")
+    if interleaved:
+        q[..., 0::2] = 1
+    else:
+        q[..., :n] = 1
+    y = f64(asp.rotate_heads(q, None, gpu(pos), gpu(f), interleaved=interleaved))[:, 0, 0]
+    got = (y[:, 0::2], y[:, 1::2]) if interleaved else (y[:, :n], y[:, n:])
+    a = pos[:, None].astype(np.longdouble) * f
+    for x, want in zip(got, (np.cos(a), np.sin(a))):
+        # a unit is at most 2^-23 of a number; angles are products of three roundings of 2^-53
+        assert (np.abs(x - want) <= 2 * 2.0 ** -23 * np.abs(want) + 4 * 2.0 ** -53 * np.abs(a)).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("B,R,H,Hk,D,n", [
