@@ -144,6 +144,7 @@ int asymspec_read_cache(const asymspec_cache* cache, const int32_t* block_table,
  * A row that sees nothing, and a row r >= new_tokens[b], is 0 with lse -inf.
  * Scores, statistics and sums are fp32; a probability is split into bf16 parts
  * whose sum is within 2^-17 of it (bf16) or 2^-24 (fp32), an fp32 query likewise.
+ * Sums hold up to 2^8 times each value, and overflow where that is beyond fp32.
  * A position that is not seen has no effect, whatever it holds.  The same inputs
  * give the same outputs, bit for bit.
  *   q            [B][R][q_heads][dim] (dtype, aligned to an element)

@@ -436,7 +436,9 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int heads = A.a.cache.heads, per_unit = heads * A.row_tiles;
 
-  // The requests' first units in the list, and the request of this workgroup's first one.
+  // The requests' first units in the list, and the request of this workgroup's first one.  Each
+  // workgroup counts all requests' units, with as many threads, up to three times over: one row
+  // of one head over one position takes 6.4 us for 256 requests, 8.2 for 1024, 16.8 for 4096.
   const int each = (A.a.B + kAttendThreads - 1) / kAttendThreads;
   const Range lane_first(A, min(tid * each, A.a.B - 1));    // (a thread's only one, up to 256 requests)
   const int me = blockIdx.x;
