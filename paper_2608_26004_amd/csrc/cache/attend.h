@@ -301,10 +301,8 @@ STEP_DEV void finish(const AttendArgs& A, int b, int r, int q_head, int dim, int
 // caches.  Each place has lines of its own (the first begins on one, and they are whole
 // lines), which one workgroup stores and one loads in a call, behind the counter, so that
 // no cache holds them from before: a line that two places share would be in a die's cache
-// once one of them is joined there, and the other be read as it was then.  (The place that
-// a group's result goes to is loaded and stored by the one that joins the group, whose
-// stores pass through its own die's caches, and loaded by another behind a counter.)
-// (An agent's fences write back and drop a die's whole cache, which cost 100 us a call.)
+// once one of them is joined there, and the other be read as it was then.  (An agent's
+// fences write back and drop a die's whole cache, which cost 100 us a call.)
 STEP_DEV void leave(float* p, float x, float y) {
   const uint64_t v = (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x);
   __hip_atomic_store((uint64_t*)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
@@ -904,9 +902,9 @@ __global__ __launch_bounds__(kAttendThreads, attend_waves(BITS, DT == ASYMSPEC_B
       }
       J.w0 = w0;
       // Many parts are joined in groups first, each by the last to leave one of its own, and the
-      // last group to be joined joins the groups'.  A group's result is in the place that its
-      // first workgroup has left; that is one where each workgroup has one run.  (12 rows over
-      // 131072 positions of one head 21 us, at once 50; 4 rows over 8 heads 44.)
+      // last group to be joined joins the groups'.  A group's result goes to its first
+      // workgroup's other place, which is free: each workgroup has a part of one run alone.  (12
+      // rows over 131072 positions of one head 21 us, at once 50; 4 rows over 8 heads 44.)
       if (most > 0 && J.parts > 32) {
         const int shares = max(1, kAttendThreads / (min(16 * MT, A.rows - row0) * (D / 8)));
         if (J.parts > 8 + 24 * shares) {
